@@ -66,6 +66,9 @@ struct GemmParams {
     int64_t ldr = 0, rows_pad = 0;
     double* sq_part = nullptr;    // [mxfp4_gemm_workgroups]
     int scales_aligned;       // both scale arrays 4-byte aligned
+    // gathered tiles only: row m of the product is row rows[m] of the a_rows rows of A
+    const int32_t* rows = nullptr;
+    int64_t a_rows = 0;
 };
 
 hipError_t launch(Kind kind, int a, const Params& p, Mapping map, hipStream_t st);
