@@ -43,6 +43,7 @@
 #ifndef KROQUANT_H
 #define KROQUANT_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -227,6 +228,125 @@ kq_status kq_mxfp4_gemm(const uint8_t* a_codes, const uint8_t* a_scales, int64_t
  */
 kq_status kq_mxfp4_gemm_bf16(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
                              const uint8_t* b_scales, int64_t N, int64_t K, uint16_t* C, int64_t ldc, void* stream);
+
+/* Type of an array that a call takes in two types. */
+typedef enum kq_dtype { KQ_DTYPE_FP32 = 0, KQ_DTYPE_BF16 = 1 } kq_dtype;
+
+/* Activation of a linear layer's epilogue. */
+typedef enum kq_act {
+    KQ_ACT_NONE = 0,
+    KQ_ACT_GELU = 1,      /* p (1 + erf(p / sqrt 2)) / 2                                  */
+    KQ_ACT_GELU_TANH = 2, /* p (1 + tanh(sqrt(2 / pi) (p + 0.044715 p^3))) / 2            */
+    KQ_ACT_SILU = 3,      /* p / (1 + exp(-p))                                            */
+    KQ_ACT_RELU = 4,
+    KQ_ACT_SWIGLU = 5     /* silu(p_2j) p_2j+1: N / 2 columns from N, N even               */
+} kq_act;
+
+/*
+ * kq_mxfp4_linear -- kq_mxfp4_gemm with what follows it in its epilogue, so
+ * that the product never goes to memory:
+ *     out = residual + gate act(deq(A) deq(B)^T + bias)
+ * Products, sums and the epilogue are in 32 bits; out is rounded once.
+ *   a_*, b_*  operands as for kq_mxfp4_gemm (M, N and K too)
+ *   bias      [N] or NULL
+ *   gate      or NULL: rows b gate_rows .. (b + 1) gate_rows - 1 of out are
+ *             multiplied by the vector of No values at gate + b * gate_stride
+ *             elements (a slice of a modulation tensor, or one vector with
+ *             gate_rows = M); gate_rows >= 1
+ *   vec_dtype type of bias and gate
+ *   act       as above; No = N / 2 for KQ_ACT_SWIGLU, else N
+ *   residual  [M, ldr] or NULL, of out's type; it may be out itself
+ *   out       [M, ldo], ldo >= No, of out_dtype
+ * Arrays are aligned to their elements, codes to 16 bytes.  N may be at most
+ * 65535 * 128 and K 2^30.  M, N = 0 is a no-op.  Enqueued on `stream`; no
+ * allocation, no synchronization.
+ */
+kq_status kq_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
+                          const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
+                          int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act,
+                          const void* residual, int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream);
+
+/*
+ * kq_mxfp4_grouped_linear -- kq_mxfp4_linear's product grouped by expert, on
+ * ragged groups whose sizes are on the device only:
+ *     out[r] = row_scale[r] act(deq(A)[rows[r]] deq(B_e)^T + bias_e)
+ * for every expert e and r = offsets[e] .. offsets[e + 1] - 1.
+ *   a_codes   [a_rows, K/2], a_scales [a_rows, K/32]: the tokens
+ *   rows      device int32 [R]: the token of each row (rows gathered while
+ *             they are loaded), or NULL: row r is token r (then R <= a_rows)
+ *   b_codes   [E, N, K/2], b_scales [E, N, K/32]: the experts' weights
+ *   offsets   device int32 [E + 1], not decreasing, within 0 .. R.  Rows of out
+ *             before offsets[0] and from offsets[E] on are not written.
+ *             (Nothing outside the arrays is touched for other offsets or
+ *             rows: they are taken as the nearest ones inside.)
+ *   bias      [E, N] or NULL, of vec_dtype
+ *   row_scale device fp32 [R] or NULL: the router's weights
+ *   out       [R, ldo] of out_dtype, as for kq_mxfp4_linear
+ * R and a_rows are at most 2^31 - 1.  R, N, E = 0 is a no-op.  Enqueued on `stream`; no
+ * allocation, no synchronization.
+ */
+kq_status kq_mxfp4_grouped_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t a_rows, const int32_t* rows,
+                                  int64_t R, const uint8_t* b_codes, const uint8_t* b_scales, int64_t E, int64_t N,
+                                  int64_t K, const int32_t* offsets, const void* bias, kq_dtype vec_dtype, kq_act act,
+                                  const float* row_scale, void* out, int64_t ldo, kq_dtype out_dtype, void* stream);
+
+/* Kind of a norm over a row of d values: v / sqrt(mean v^2 + eps), or of v - mean v. */
+typedef enum kq_norm { KQ_NORM_NONE = 0, KQ_NORM_RMS = 1, KQ_NORM_LAYER = 2 } kq_norm;
+
+/*
+ * kq_block_norm -- the residual stream's update and the norm before the next
+ * block in one pass (the AdaLN or pre-norm whose output the quantizers take):
+ *     u = x, or norm(x) post_weight          (post_norm: a norm behind the block)
+ *     h = residual + alpha gate u
+ *     y = norm(h) weight (1 + scale) + shift (of the 32-bit h, before its rounding)
+ *   x            [M, d] of x_dtype: the block's output
+ *   residual, h  [M, d] of stream_dtype; residual may be NULL (0), and h NULL
+ *                (not written).  They may be the same array.
+ *   gate, scale, shift  vectors of d values for each of `batches` batches of
+ *                M / batches rows (batches divides M), batch b's at
+ *                b * its stride elements; each may be NULL
+ *   weight, post_weight  [d] or NULL (post_weight only with a post_norm)
+ *   vec_dtype    type of all vectors
+ *   norm         of y; KQ_NORM_NONE: no y (then y must be NULL)
+ *   y            [M, d] of x_dtype; it may be x itself
+ * Sums are in 32 bits, the mean is subtracted before the squares are summed.
+ * d is 1 to 16384, eps >= 0; arrays are aligned to their elements.  M = 0 is a no-op.  Enqueued
+ * on `stream`; no allocation, no synchronization.
+ */
+kq_status kq_block_norm(const void* x, kq_dtype x_dtype, const void* residual, kq_dtype stream_dtype, int64_t M, int64_t d,
+                        int64_t batches, const void* gate, int64_t gate_stride, const void* scale, int64_t scale_stride,
+                        const void* shift, int64_t shift_stride, const void* weight, const void* post_weight,
+                        kq_dtype vec_dtype, kq_norm norm, kq_norm post_norm, float alpha, float eps, void* h, void* y,
+                        void* stream);
+
+/* Bytes of device workspace that kq_block_norm_backward needs for these sizes. */
+kq_status kq_block_norm_workspace_size(int64_t M, int64_t d, int64_t batches, size_t* bytes);
+
+/*
+ * kq_block_norm_backward -- the gradients of kq_block_norm's inputs from dy
+ * (x_dtype) and dh (stream_dtype; the gradient that comes back along the
+ * stream, or NULL for 0).  h is the array that kq_block_norm wrote, x its
+ * input; the norms are computed again from them.
+ *   x          may be NULL without a post_norm and without dgate
+ *   gate, scale, weight, post_weight, norms, alpha, eps: as in the forward call
+ *   dx         [M, d] of x_dtype or NULL;  dresidual [M, d] of stream_dtype or NULL
+ *              (the gradient of h)
+ *   dgate, dscale, dshift  fp32 [batches, d] or NULL (dgate and dscale also
+ *              where gate and scale are NULL: the gradients at 1 and at 0)
+ *   dweight, dpost_weight  fp32 [d] or NULL
+ *   workspace  device, 16-byte aligned, kq_block_norm_workspace_size bytes; its
+ *              contents are scratch between calls
+ * dresidual may be dh and dx may be dy.  Column sums are taken in a fixed order.
+ * Enqueued on `stream`; no allocation, no synchronization.  M = 0 is a no-op (the
+ * vectors' gradients are not written).
+ */
+kq_status kq_block_norm_backward(const void* dy, const void* dh, const void* x, kq_dtype x_dtype, const void* h,
+                                 kq_dtype stream_dtype, int64_t M, int64_t d, int64_t batches, const void* gate,
+                                 int64_t gate_stride, const void* scale, int64_t scale_stride, const void* weight,
+                                 const void* post_weight, kq_dtype vec_dtype, kq_norm norm, kq_norm post_norm,
+                                 float alpha, float eps, void* dx, void* dresidual, float* dgate, float* dscale,
+                                 float* dshift, float* dweight, float* dpost_weight, void* workspace,
+                                 size_t workspace_bytes, void* stream);
 
 /*
  * kq_mxfp4_quantize -- the bare MXFP4 quantizer ("Q4", the lower bound of

@@ -4,13 +4,15 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkroquant.so")
 BIND = os.path.join(PKG, "_kqbind.so")  # native marshalling of the Python binding
-SOURCES = ["kq_kernels.hip", "kq_gemm.hip", "kq_calib.hip", "kq_api.hip"]
+SOURCES = ["kq_kernels.hip", "kq_gemm.hip", "kq_linear.hip", "kq_norm.hip", "kq_calib.hip", "kq_api.hip"]
 
 # -packed-fp32-ops off: no v_pk_{add,mul,fma}_f32 in the device code.
 # -ffp-contract=off: only the explicit fmaf calls fuse, which keeps the
@@ -53,9 +55,11 @@ def build_bind(verbose: bool = False) -> str:
 
 def build(verbose: bool = False) -> str:
     """Compile every HIP source into libkroquant.so (always recompiles), then the binding's native part."""
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB + ".tmp"]
-    _run(cmd, verbose)
+    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        list(pool.map(lambda s, o: _run([*cmd, "-c", os.path.join(CSRC, s), "-o", o], verbose), SOURCES, objects))
+        _run([*cmd, *objects, "-o", LIB + ".tmp"], verbose)
     os.replace(LIB + ".tmp", LIB)
     build_bind(verbose)
     return LIB

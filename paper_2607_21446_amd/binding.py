@@ -33,6 +33,8 @@ EXPORTED = (
     "kq_e2m1_encode", "kq_weight_transform", "kq_factors_inverse_transpose", "kq_lu_to_factors",
     "kq_calib_workspace_size", "kq_calib_reference", "kq_calib_step", "kq_calibrate",
     "kq_calib_step_noalloc",
+    "kq_mxfp4_linear", "kq_mxfp4_grouped_linear", "kq_block_norm", "kq_block_norm_workspace_size",
+    "kq_block_norm_backward",
     "kq_status_string", "kq_last_error_detail", "kq_version",
 )
 
@@ -76,7 +78,13 @@ def lib() -> ctypes.CDLL:
     L.kq_calibrate.argtypes = [P, I64, I64, P, I64, P, P, I, I64, I, F, P, P, ctypes.c_size_t, P]
     L.kq_calib_step_noalloc.argtypes = [P, I64, I64, P, I64, P, P, I, I64, P, P, P, P, P, I, F, P]
     L.kq_timestamp.argtypes = [P, P]
-    for name in EXPORTED[:23]:
+    L.kq_mxfp4_linear.argtypes = [P, P, I64, P, P, I64, I64, P, P, I64, I64, I, I, P, I64, P, I64, I, P]
+    L.kq_mxfp4_grouped_linear.argtypes = [P, P, I64, P, I64, P, P, I64, I64, I64, P, P, I, I, P, P, I64, I, P]
+    L.kq_block_norm.argtypes = [P, I, P, I, I64, I64, I64, P, I64, P, I64, P, I64, P, P, I, I, I, F, F, P, P, P]
+    L.kq_block_norm_workspace_size.argtypes = [I64, I64, I64, ctypes.POINTER(ctypes.c_size_t)]
+    L.kq_block_norm_backward.argtypes = [P, P, P, I, P, I, I64, I64, I64, P, I64, P, I64, P, P, I, I, I, F, F, P, P, P, P,
+                                         P, P, P, P, ctypes.c_size_t, P]
+    for name in EXPORTED[:-3]:
         getattr(L, name).restype = ctypes.c_int
     L.kq_status_string.argtypes = [I]
     L.kq_status_string.restype = ctypes.c_char_p
@@ -343,6 +351,266 @@ def mxfp4_gemm(a_codes, a_scales, b_codes, b_scales, C=None, accumulate=False, s
     _check(lib().kq_mxfp4_gemm(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(C),
                                C.stride(0), int(accumulate), _stream(stream)), "kq_mxfp4_gemm")
     return C
+
+
+_FLOATS = {torch.float32: 0, torch.bfloat16: 1}  # kq_dtype
+_ACTS = {None: 0, "gelu": 1, "gelu_tanh": 2, "silu": 3, "relu": 4, "swiglu": 5}  # kq_act
+_NORMS = {None: 0, "rms": 1, "layer": 2}  # kq_norm
+
+
+def _one_of(table, key, name):
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        raise ValueError(f"{name} must be one of {', '.join(map(str, table))}, got {key!r}") from None
+
+
+def _float(t, name, dtype=None):
+    """A device tensor of a type that the call takes, or of exactly ``dtype``."""
+    if t.dtype not in _FLOATS or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be {dtype or 'float32 or bfloat16'}, got {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+
+
+def _rows_of(t, shape, name, device, dtype=None):
+    """A matrix whose rows are contiguous (they may lie apart): its row stride."""
+    _float(t, name, dtype)
+    if tuple(t.shape) != tuple(shape) or t.device != device:
+        raise ValueError(f"{name} must be {list(shape)} on {device}, got {list(t.shape)} on {t.device}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if shape[0] > 1 and t.stride(0) < shape[1]:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _vectors(named, d, device):
+    """Vectors of one type, [d] or one for each of B batches [B, d] (rows contiguous, any stride between
+    them): kq_dtype, B and the strides.  ``named``: (name, tensor or None, per batch) in order."""
+    dtype, batches, strides = None, None, []
+    for name, t, per_batch in named:
+        strides.append(0)
+        if t is None:
+            continue
+        _float(t, name, dtype)
+        dtype = t.dtype
+        if t.device != device or t.dim() not in ((1, 2) if per_batch else (1,)) or t.shape[-1] != d or (d > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name} must be {'[B, ' if per_batch else '['}{d}] with contiguous rows on {device}, "
+                             f"got {list(t.shape)} on {t.device}")
+        if per_batch:
+            n = t.shape[0] if t.dim() == 2 else 1
+            if batches not in (None, n):
+                raise ValueError(f"{name} has {n} batches, the others {batches}")
+            batches = n
+            strides[-1] = t.stride(0) if t.dim() == 2 else 0
+            if strides[-1] < 0:
+                raise ValueError(f"{name} must not have a negative stride")
+    return 0 if dtype is None else _FLOATS[dtype], 1 if batches is None else batches, strides
+
+
+def _batches(M, batches):
+    if batches < 1 or M % batches:
+        raise ValueError(f"{batches} batches do not divide {M} rows")
+
+
+def _linear_out(out, rows, cols, out_dtype, device):
+    if out is None:
+        out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=device)
+    return out, _rows_of(out, (rows, cols), "out", device)
+
+
+def _mxfp4_operands(a_codes, a_scales, b_codes, b_scales, experts):
+    for t, name in ((a_codes, "a_codes"), (a_scales, "a_scales"), (b_codes, "b_codes"), (b_scales, "b_scales")):
+        _need(t, torch.uint8, name)
+    M, K = _matrix(a_codes, "a_codes")[0], 2 * a_codes.shape[1]
+    if b_codes.dim() != (3 if experts else 2):
+        raise ValueError(f"b_codes must be {'[E, N, K/2]' if experts else '[N, K/2]'}, got shape {tuple(b_codes.shape)}")
+    lead, N = tuple(b_codes.shape[:-1]), b_codes.shape[-2]
+    if b_codes.shape[-1] * 2 != K or a_scales.shape != (M, K // 32) or b_scales.shape != (*lead, K // 32):
+        raise ValueError("operand shapes do not match")
+    if any(t.device != a_codes.device for t in (a_scales, b_codes, b_scales)):
+        raise ValueError("all operands must be on one device")
+    return M, N, K
+
+
+def mxfp4_linear(a_codes, a_scales, b_codes, b_scales, bias=None, act=None, gate=None, residual=None, out=None,
+                 out_dtype=None, stream=None):
+    """kq_mxfp4_linear: out = residual + gate * act(deq(A) deq(B)^T + bias) for
+    MXFP4 operands as for mxfp4_gemm.  ``act``: None, "gelu", "gelu_tanh", "silu",
+    "relu" or "swiglu" (columns 2j, 2j + 1 -> silu(p_2j) p_2j+1, half as many
+    outputs).  bias [N], gate [N'] or [B, N'] (one for each of B equal batches of
+    rows), both fp32 or both bf16; residual and out [M, N'] of one type, rows
+    apart if need be, out bf16 unless ``out_dtype`` says fp32; out may be residual.
+    Returns out."""
+    a = _one_of(_ACTS, act, "act")
+    r = _native().mxfp4_linear(a_codes, a_scales, b_codes, b_scales, bias, a, gate, residual, out, out_dtype, stream)
+    if r is not None:
+        return r
+    M, N, K = _mxfp4_operands(a_codes, a_scales, b_codes, b_scales, False)
+    if act == "swiglu" and N % 2:
+        raise ValueError(f"swiglu needs an even number of columns, got {N}")
+    dev, cols = a_codes.device, N // 2 if act == "swiglu" else N
+    vec = _vectors([("bias", bias, False)], N, dev)[0]
+    gvec, B, strides = _vectors([("gate", gate, True)], cols, dev)
+    if bias is not None and gate is not None and vec != gvec:
+        raise TypeError(f"bias and gate must have one type, got {bias.dtype} and {gate.dtype}")
+    _batches(M, B)
+    if out is None and out_dtype is None and residual is not None:
+        out_dtype = residual.dtype
+    out, ldo = _linear_out(out, M, cols, out_dtype, dev)
+    ldr = 0 if residual is None else _rows_of(residual, (M, cols), "residual", dev, out.dtype)
+    _check(lib().kq_mxfp4_linear(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(bias),
+                                 _ptr(gate), strides[0], max(1, M // B), vec if gate is None else gvec, a, _ptr(residual), ldr,
+                                 _ptr(out), ldo, _FLOATS[out.dtype], _stream(stream)), "kq_mxfp4_linear")
+    return out
+
+
+def mxfp4_grouped_linear(a_codes, a_scales, b_codes, b_scales, offsets, rows=None, bias=None, act=None, row_scale=None,
+                         out=None, out_dtype=None, stream=None):
+    """kq_mxfp4_grouped_linear: row r of out, offsets[e] <= r < offsets[e + 1], is
+    row_scale[r] * act(deq(A)[rows[r]] deq(B_e)^T + bias[e]).  b_codes [E, N, K/2],
+    b_scales [E, N, K/32]; offsets int32 [E + 1] and rows int32 [R] (without it,
+    row r of A) on the device; row_scale fp32 [R]; bias [E, N] fp32 or bf16.  Rows of
+    a given ``out`` that no group has are left as they are; those of a new one are
+    unspecified.  Returns out [R, N'] (bf16 unless ``out_dtype`` says fp32)."""
+    a = _one_of(_ACTS, act, "act")
+    r = _native().mxfp4_grouped_linear(a_codes, a_scales, b_codes, b_scales, offsets, rows, bias, a, row_scale, out,
+                                       out_dtype, stream)
+    if r is not None:
+        return r
+    T, N, K = _mxfp4_operands(a_codes, a_scales, b_codes, b_scales, True)
+    if act == "swiglu" and N % 2:
+        raise ValueError(f"swiglu needs an even number of columns, got {N}")
+    dev, E, cols = a_codes.device, b_codes.shape[0], N // 2 if act == "swiglu" else N
+    _need(offsets, torch.int32, "offsets")
+    _size(offsets, E + 1, "offsets", dev)
+    R = T
+    if rows is not None:
+        _need(rows, torch.int32, "rows")
+        R = rows.numel()
+        _size(rows, R, "rows", dev)
+    if bias is not None:
+        _float(bias, "bias")
+        if bias.shape != (E, N) or bias.device != dev or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous [{E}, {N}] on {dev}, got {list(bias.shape)} on {bias.device}")
+    if row_scale is not None:
+        _need(row_scale, torch.float32, "row_scale")
+        _size(row_scale, R, "row_scale", dev)
+    out, ldo = _linear_out(out, R, cols, out_dtype, dev)
+    _check(lib().kq_mxfp4_grouped_linear(_ptr(a_codes), _ptr(a_scales), T, _ptr(rows), R, _ptr(b_codes), _ptr(b_scales),
+                                         E, N, K, _ptr(offsets), _ptr(bias), 0 if bias is None else _FLOATS[bias.dtype], a,
+                                         _ptr(row_scale), _ptr(out), ldo, _FLOATS[out.dtype], _stream(stream)),
+           "kq_mxfp4_grouped_linear")
+    return out
+
+
+def _same(t, like, name, dtype=None):
+    _float(t, name, dtype or like.dtype)
+    if t.shape != like.shape or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(like.shape)} on {like.device}, got {list(t.shape)} on {t.device}")
+
+
+def block_norm(x, residual=None, gate=None, post_weight=None, weight=None, scale=None, shift=None, norm="layer",
+               post_norm=None, alpha=1.0, eps=1e-6, h=None, y=None, h_dtype=None, stream=None):
+    """kq_block_norm: h = residual + alpha * gate * u and
+    y = norm(h) * weight * (1 + scale) + shift, with u = x or, with a
+    ``post_norm``, norm(x) * post_weight.  Norms: "layer", "rms" (``norm`` may be
+    None: no y).  x [M, d] fp32 or bf16, y of its type; residual and h [M, d] of
+    another of the two if need be (h of residual's type, else ``h_dtype``, else x's).
+    gate, scale and shift [d] or [B, d] for B equal batches of rows (slices of one
+    modulation tensor), weight and post_weight [d], all of one type.  h may be
+    residual and y may be x.  Where h would be x itself it is not written, and x
+    is returned for it.  Returns (h, y)."""
+    kind, post = _one_of(_NORMS, norm, "norm"), _one_of(_NORMS, post_norm, "post_norm")
+    r = _native().block_norm(x, residual, gate, post_weight, weight, scale, shift, kind, post, alpha, eps, h, y, h_dtype,
+                             stream)
+    if r is not None:
+        return r
+    _float(x, "x")
+    M, d = _matrix(x, "x")
+    _same(x, x, "x")
+    vec, B, st = _vectors([("gate", gate, True), ("scale", scale, True), ("shift", shift, True), ("weight", weight, False),
+                           ("post_weight", post_weight, False)], d, x.device)
+    _batches(M, B)
+    if residual is not None:
+        _same(residual, x, "residual", residual.dtype)
+        h_dtype = residual.dtype
+    plain = residual is None and gate is None and not post and alpha == 1.0 and h is None and h_dtype in (None, x.dtype)
+    if h is None and not plain:
+        h = torch.empty((M, d), dtype=h_dtype or x.dtype, device=x.device)
+    if h is not None:
+        _same(h, x, "h", h.dtype if residual is None else residual.dtype)
+    if y is None and kind:
+        y = torch.empty_like(x)
+    if y is not None:
+        _same(y, x, "y")
+    if not kind and plain:
+        return x, None
+    _check(lib().kq_block_norm(_ptr(x), _FLOATS[x.dtype], _ptr(residual), _FLOATS[x.dtype if h is None else h.dtype], M, d, B,
+                               _ptr(gate), st[0], _ptr(scale), st[1], _ptr(shift), st[2], _ptr(weight), _ptr(post_weight), vec,
+                               kind, post, float(alpha), float(eps), _ptr(h), _ptr(y), _stream(stream)), "kq_block_norm")
+    return (x if h is None else h), y
+
+
+def block_norm_workspace(M, d, batches=1, device="cuda"):
+    """Device workspace of block_norm_backward for these sizes."""
+    n = ctypes.c_size_t(0)
+    _check(lib().kq_block_norm_workspace_size(M, d, batches, ctypes.byref(n)), "kq_block_norm_workspace_size")
+    return torch.empty(int(n.value), dtype=torch.uint8, device=device)
+
+
+def block_norm_backward(dy, h, dh=None, x=None, gate=None, post_weight=None, weight=None, scale=None, shift=None,
+                        norm="layer", post_norm=None, alpha=1.0, eps=1e-6, dx=None, dresidual=None, workspace=None,
+                        stream=None):
+    """kq_block_norm_backward: gradients of block_norm from dy (of y's type) and dh
+    (of h's, the gradient that comes back along the stream; None: zero).  h is what
+    block_norm returned, x its input (needed with a gate or a ``post_norm``); the
+    vectors are the forward call's (shift is asked for its gradient only).  Returns a
+    dict: dx, dresidual, and fp32 dgate, dscale, dshift (the vectors' shapes),
+    dweight, dpost_weight for the vectors that are given."""
+    kind, post = _one_of(_NORMS, norm, "norm"), _one_of(_NORMS, post_norm, "post_norm")
+    if not kind:
+        raise ValueError("the backward pass needs a norm")
+    _float(dy, "dy")
+    M, d = _matrix(dy, "dy")
+    _same(dy, dy, "dy")
+    _same(h, dy, "h", h.dtype)
+    if dh is not None:
+        _same(dh, h, "dh")
+    if x is not None:
+        _same(x, dy, "x")
+    elif post or gate is not None:
+        raise ValueError("a gate or a post_norm needs x")
+    vec, B, st = _vectors([("gate", gate, True), ("scale", scale, True), ("shift", shift, True), ("weight", weight, False),
+                           ("post_weight", post_weight, False)], d, dy.device)
+    _batches(M, B)
+    # without a gate, a post norm and a factor both gradients are one array
+    one = gate is None and not post and alpha == 1.0 and h.dtype == dy.dtype and dx is None
+    if dresidual is None:
+        dresidual = torch.empty_like(h)
+    _same(dresidual, h, "dresidual")
+    if dx is None and not one:
+        dx = torch.empty_like(dy)
+    if dx is not None:
+        _same(dx, dy, "dx")
+    if workspace is None:
+        workspace = block_norm_workspace(M, d, B, dy.device)
+    _need(workspace, torch.uint8, "workspace")
+    if workspace.device != dy.device:
+        raise ValueError(f"workspace is on {workspace.device}, the input on {dy.device}")
+    make = torch.empty if M else torch.zeros
+    out = {}
+    for name, t in (("dgate", gate), ("dscale", scale), ("dshift", shift), ("dweight", weight), ("dpost_weight", post_weight)):
+        if t is not None:
+            out[name] = make(t.shape, dtype=torch.float32, device=dy.device)
+    if M:
+        _check(lib().kq_block_norm_backward(
+            _ptr(dy), _ptr(dh), _ptr(x), _FLOATS[dy.dtype], _ptr(h), _FLOATS[h.dtype], M, d, B, _ptr(gate), st[0], _ptr(scale),
+            st[1], _ptr(weight), _ptr(post_weight), vec, kind, post, float(alpha), float(eps), _ptr(dx), _ptr(dresidual),
+            *(_ptr(out.get(n)) for n in ("dgate", "dscale", "dshift", "dweight", "dpost_weight")), _ptr(workspace),
+            workspace.numel(), _stream(stream)), "kq_block_norm_backward")
+    return {"dx": dresidual if dx is None else dx, "dresidual": dresidual, **out}
 
 
 def mxfp4(X, codes=None, scales=None, stream=None):

@@ -15,6 +15,8 @@
 
 #include "kq_calib.h"
 #include "kq_kernels.h"
+#include "kq_linear.h"
+#include "kq_norm.h"
 #include "kroquant.h"
 
 namespace {
@@ -366,6 +368,233 @@ kq_status kq_mxfp4_gemm_bf16(const uint8_t* a_codes, const uint8_t* a_scales, in
     kq::GemmParams g = gemm_params(a_codes, a_scales, M, b_codes, b_scales, N, K, nullptr, ldc, 0, nullptr);
     g.C16 = C;
     return from_hip(kq::launch_mxfp4_gemm(g, (hipStream_t)stream), "kq_mxfp4_gemm_bf16");
+}
+
+static bool dtype_ok(int t) { return t == KQ_DTYPE_FP32 || t == KQ_DTYPE_BF16; }
+static size_t dtype_bytes(int t) { return t == KQ_DTYPE_BF16 ? 2 : 4; }
+
+// Sizes, types and pointers that both linear layers share.  rows: of out.
+static kq_status check_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t rows, const uint8_t* b_codes,
+                              const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, int vec_dtype, int act,
+                              const void* out, int64_t ldo, int out_dtype) {
+    if (rows < 0 || N < 0) return fail(KQ_ERROR_INVALID_VALUE, "rows = %lld and N = %lld must be >= 0", (long long)rows, (long long)N);
+    if (K <= 0 || K % 32 != 0) return fail(KQ_ERROR_INVALID_VALUE, "K = %lld must be a positive multiple of 32", (long long)K);
+    if (K > (int64_t(1) << 30)) return fail(KQ_ERROR_INVALID_VALUE, "K = %lld is too large (at most 2^30)", (long long)K);
+    if (rows > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "%lld rows are too many (at most 2^31 - 1)", (long long)rows);
+    if (N > 65535 * 128) return fail(KQ_ERROR_INVALID_VALUE, "N = %lld is too large (at most 65535 * 128)", (long long)N);
+    if (!dtype_ok(vec_dtype) || !dtype_ok(out_dtype)) return fail(KQ_ERROR_INVALID_VALUE, "vec_dtype and out_dtype must be a kq_dtype");
+    if (act < KQ_ACT_NONE || act > KQ_ACT_SWIGLU) return fail(KQ_ERROR_INVALID_VALUE, "act = %d must be a kq_act", act);
+    if (act == KQ_ACT_SWIGLU && N % 2) return fail(KQ_ERROR_INVALID_VALUE, "N = %lld must be even with KQ_ACT_SWIGLU", (long long)N);
+    const int64_t cols = act == KQ_ACT_SWIGLU ? N / 2 : N;
+    if (ldo < cols) return fail(KQ_ERROR_INVALID_VALUE, "ldo = %lld must be >= %lld", (long long)ldo, (long long)cols);
+    if (rows == 0 || N == 0) return ok();
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out)
+        return fail(KQ_ERROR_NULL_POINTER, "codes, scales and out must not be NULL");
+    if (!aligned(a_codes, 16) || !aligned(b_codes, 16)) return fail(KQ_ERROR_MISALIGNED, "codes must be 16-byte aligned");
+    if (!aligned(bias, dtype_bytes(vec_dtype)) || !aligned(out, dtype_bytes(out_dtype)))
+        return fail(KQ_ERROR_MISALIGNED, "bias and out must be aligned to their elements");
+    return ok();
+}
+
+static kq::LinearParams linear_params(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
+                                      const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, int vec_dtype,
+                                      int act, void* out, int64_t ldo, int out_dtype) {
+    kq::LinearParams p{};
+    p.g = gemm_params(a_codes, a_scales, M, b_codes, b_scales, N, K, nullptr, 0, 0, nullptr);
+    p.act = static_cast<kq::Act>(act);
+    p.vec16 = vec_dtype == KQ_DTYPE_BF16;
+    p.out16 = out_dtype == KQ_DTYPE_BF16;
+    p.bias = bias;
+    p.out = out;
+    p.ldo = ldo;
+    return p;
+}
+
+kq_status kq_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
+                          const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
+                          int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act, const void* residual,
+                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream) {
+    const kq_status st = check_linear(a_codes, a_scales, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    if (st != KQ_SUCCESS) return st;
+    const int64_t cols = act == KQ_ACT_SWIGLU ? N / 2 : N;
+    if (gate && (gate_rows < 1 || gate_stride < 0))
+        return fail(KQ_ERROR_INVALID_VALUE, "gate_rows = %lld must be >= 1 and gate_stride = %lld >= 0", (long long)gate_rows, (long long)gate_stride);
+    if (residual && ldr < cols) return fail(KQ_ERROR_INVALID_VALUE, "ldr = %lld must be >= %lld", (long long)ldr, (long long)cols);
+    if (!aligned(gate, dtype_bytes(vec_dtype)) || !aligned(residual, dtype_bytes(out_dtype)))
+        return fail(KQ_ERROR_MISALIGNED, "gate and residual must be aligned to their elements");
+    if (M == 0 || N == 0) return ok();
+    kq::LinearParams p = linear_params(a_codes, a_scales, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    p.gate = gate;
+    p.gate_stride = gate_stride;
+    p.gate_rows = gate ? gate_rows : 1;
+    p.residual = residual;
+    p.ldr = ldr;
+    return from_hip(kq::launch_mxfp4_linear(p, (hipStream_t)stream), "kq_mxfp4_linear");
+}
+
+kq_status kq_mxfp4_grouped_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t a_rows, const int32_t* rows,
+                                  int64_t R, const uint8_t* b_codes, const uint8_t* b_scales, int64_t E, int64_t N,
+                                  int64_t K, const int32_t* offsets, const void* bias, kq_dtype vec_dtype, kq_act act,
+                                  const float* row_scale, void* out, int64_t ldo, kq_dtype out_dtype, void* stream) {
+    const kq_status st = check_linear(a_codes, a_scales, R, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    if (st != KQ_SUCCESS) return st;
+    if (E < 0 || a_rows < 0) return fail(KQ_ERROR_INVALID_VALUE, "E = %lld and a_rows = %lld must be >= 0", (long long)E, (long long)a_rows);
+    if (a_rows > INT32_MAX || E > INT32_MAX - 64)
+        return fail(KQ_ERROR_INVALID_VALUE, "a_rows = %lld or E = %lld is too large (at most 2^31 - 65)", (long long)a_rows, (long long)E);
+    if (R == 0 || N == 0 || E == 0) return ok();
+    if (!offsets) return fail(KQ_ERROR_NULL_POINTER, "offsets must not be NULL");
+    if (!aligned(offsets, 4) || !aligned(rows, 4) || !aligned(row_scale, 4))
+        return fail(KQ_ERROR_MISALIGNED, "offsets, rows and row_scale must be 4-byte aligned");
+    if (a_rows == 0 || (!rows && R > a_rows))
+        return fail(KQ_ERROR_INVALID_VALUE, "R = %lld rows from a_rows = %lld need an index", (long long)R, (long long)a_rows);
+    kq::LinearParams p = linear_params(a_codes, a_scales, R, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    p.g.rows = rows;
+    p.g.a_rows = a_rows;
+    p.offsets = offsets;
+    p.experts = E;
+    p.row_scale = row_scale;
+    if (kq::mxfp4_grouped_workgroups(p) > INT32_MAX)
+        return fail(KQ_ERROR_UNSUPPORTED, "R = %lld, E = %lld and N = %lld need more workgroups than one launch holds", (long long)R,
+                    (long long)E, (long long)N);
+    return from_hip(kq::launch_mxfp4_linear(p, (hipStream_t)stream), "kq_mxfp4_grouped_linear");
+}
+
+static kq_status check_norm(int64_t M, int64_t d, int64_t batches, int x_dtype, int stream_dtype, int vec_dtype, int norm,
+                            int post, float eps) {
+    if (M < 0 || M > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "M = %lld must be in [0, 2^31 - 1]", (long long)M);
+    if (d < 1 || d > kq::kNormMaxColumns)
+        return fail(KQ_ERROR_INVALID_VALUE, "d = %lld must be in [1, %lld]", (long long)d, (long long)kq::kNormMaxColumns);
+    if (batches < 1 || M % batches) return fail(KQ_ERROR_INVALID_VALUE, "batches = %lld must divide M = %lld", (long long)batches, (long long)M);
+    if (!dtype_ok(x_dtype) || !dtype_ok(stream_dtype) || !dtype_ok(vec_dtype))
+        return fail(KQ_ERROR_INVALID_VALUE, "x_dtype, stream_dtype and vec_dtype must be a kq_dtype");
+    if (norm < KQ_NORM_NONE || norm > KQ_NORM_LAYER || post < KQ_NORM_NONE || post > KQ_NORM_LAYER)
+        return fail(KQ_ERROR_INVALID_VALUE, "norm = %d and post_norm = %d must be a kq_norm", norm, post);
+    if (!(eps >= 0.0f)) return fail(KQ_ERROR_INVALID_VALUE, "eps must be >= 0");
+    return ok();
+}
+
+static kq_status check_vectors(const void* gate, int64_t gate_stride, const void* scale, int64_t scale_stride, const void* shift,
+                               int64_t shift_stride, const void* weight, const void* post_weight, int vec_dtype, int post) {
+    if ((gate && gate_stride < 0) || (scale && scale_stride < 0) || (shift && shift_stride < 0))
+        return fail(KQ_ERROR_INVALID_VALUE, "the strides of gate, scale and shift must be >= 0");
+    if (post_weight && post == KQ_NORM_NONE) return fail(KQ_ERROR_INVALID_VALUE, "post_weight needs a post_norm");
+    for (const void* v : {gate, scale, shift, weight, post_weight})
+        if (!aligned(v, dtype_bytes(vec_dtype))) return fail(KQ_ERROR_MISALIGNED, "vectors must be aligned to their elements");
+    return ok();
+}
+
+kq_status kq_block_norm(const void* x, kq_dtype x_dtype, const void* residual, kq_dtype stream_dtype, int64_t M, int64_t d,
+                        int64_t batches, const void* gate, int64_t gate_stride, const void* scale, int64_t scale_stride,
+                        const void* shift, int64_t shift_stride, const void* weight, const void* post_weight,
+                        kq_dtype vec_dtype, kq_norm norm, kq_norm post_norm, float alpha, float eps, void* h, void* y,
+                        void* stream) {
+    kq_status st = check_norm(M, d, batches, x_dtype, stream_dtype, vec_dtype, norm, post_norm, eps);
+    if (st == KQ_SUCCESS)
+        st = check_vectors(gate, gate_stride, scale, scale_stride, shift, shift_stride, weight, post_weight, vec_dtype, post_norm);
+    if (st != KQ_SUCCESS) return st;
+    if (M == 0) return ok();
+    if ((norm == KQ_NORM_NONE) != (y == nullptr))
+        return fail(y ? KQ_ERROR_INVALID_VALUE : KQ_ERROR_NULL_POINTER, "y goes with a norm: y must be NULL exactly where norm is KQ_NORM_NONE");
+    if (!x || (!h && !y)) return fail(KQ_ERROR_NULL_POINTER, "x, and h or y, must not be NULL");
+    if (!aligned(x, dtype_bytes(x_dtype)) || !aligned(y, dtype_bytes(x_dtype)) || !aligned(residual, dtype_bytes(stream_dtype)) ||
+        !aligned(h, dtype_bytes(stream_dtype)))
+        return fail(KQ_ERROR_MISALIGNED, "x, residual, h and y must be aligned to their elements");
+    kq::NormParams p{};
+    p.x = x;
+    p.residual = residual;
+    p.gate = gate;
+    p.scale = scale;
+    p.shift = shift;
+    p.gate_stride = gate_stride;
+    p.scale_stride = scale_stride;
+    p.shift_stride = shift_stride;
+    p.weight = weight;
+    p.post_weight = post_weight;
+    p.M = M;
+    p.d = d;
+    p.rows = M / batches;
+    p.norm = norm;
+    p.post = post_norm;
+    p.alpha = alpha;
+    p.eps = eps;
+    p.x16 = x_dtype == KQ_DTYPE_BF16;
+    p.stream16 = stream_dtype == KQ_DTYPE_BF16;
+    p.vec16 = vec_dtype == KQ_DTYPE_BF16;
+    p.h = h;
+    p.y = y;
+    return from_hip(kq::launch_block_norm(p, (hipStream_t)stream), "kq_block_norm");
+}
+
+static size_t norm_workspace(int64_t M, int64_t d, int64_t batches) {
+    return M == 0 ? 16 : (size_t)(batches * kq::norm_chunks(M, batches, d) * 3 * d) * sizeof(float);
+}
+
+kq_status kq_block_norm_workspace_size(int64_t M, int64_t d, int64_t batches, size_t* bytes) {
+    const kq_status st = check_norm(M, d, batches, 0, 0, 0, 0, 0, 0.0f);
+    if (st != KQ_SUCCESS) return st;
+    if (!bytes) return fail(KQ_ERROR_NULL_POINTER, "bytes must not be NULL");
+    *bytes = norm_workspace(M, d, batches);
+    return ok();
+}
+
+kq_status kq_block_norm_backward(const void* dy, const void* dh, const void* x, kq_dtype x_dtype, const void* h,
+                                 kq_dtype stream_dtype, int64_t M, int64_t d, int64_t batches, const void* gate,
+                                 int64_t gate_stride, const void* scale, int64_t scale_stride, const void* weight,
+                                 const void* post_weight, kq_dtype vec_dtype, kq_norm norm, kq_norm post_norm, float alpha,
+                                 float eps, void* dx, void* dresidual, float* dgate, float* dscale, float* dshift,
+                                 float* dweight, float* dpost_weight, void* workspace, size_t workspace_bytes, void* stream) {
+    kq_status st = check_norm(M, d, batches, x_dtype, stream_dtype, vec_dtype, norm, post_norm, eps);
+    if (st == KQ_SUCCESS)
+        st = check_vectors(gate, gate_stride, scale, scale_stride, nullptr, 0, weight, post_weight, vec_dtype, post_norm);
+    if (st != KQ_SUCCESS) return st;
+    if (norm == KQ_NORM_NONE) return fail(KQ_ERROR_INVALID_VALUE, "the backward pass needs a norm");
+    if (dpost_weight && post_norm == KQ_NORM_NONE) return fail(KQ_ERROR_INVALID_VALUE, "dpost_weight needs a post_norm");
+    if (batches > 65534) return fail(KQ_ERROR_UNSUPPORTED, "batches = %lld is too large (at most 65534)", (long long)batches);
+    if (M == 0) return ok();
+    if (!dy || !h) return fail(KQ_ERROR_NULL_POINTER, "dy and h must not be NULL");
+    if (!x && (post_norm != KQ_NORM_NONE || dgate)) return fail(KQ_ERROR_NULL_POINTER, "a post_norm and dgate need x");
+    if (!workspace) return fail(KQ_ERROR_NULL_POINTER, "workspace must not be NULL");
+    for (const void* v : {dy, x, static_cast<const void*>(dx)})
+        if (!aligned(v, dtype_bytes(x_dtype))) return fail(KQ_ERROR_MISALIGNED, "dy, x and dx must be aligned to their elements");
+    for (const void* v : {dh, h, static_cast<const void*>(dresidual)})
+        if (!aligned(v, dtype_bytes(stream_dtype))) return fail(KQ_ERROR_MISALIGNED, "dh, h and dresidual must be aligned to their elements");
+    for (const float* v : {dgate, dscale, dshift, dweight, dpost_weight})
+        if (!aligned(v, 4)) return fail(KQ_ERROR_MISALIGNED, "the vectors' gradients must be 4-byte aligned");
+    if (!aligned(workspace, 16)) return fail(KQ_ERROR_MISALIGNED, "workspace must be 16-byte aligned");
+    if (workspace_bytes < norm_workspace(M, d, batches))
+        return fail(KQ_ERROR_INVALID_VALUE, "workspace holds %zu bytes, the call needs %zu", workspace_bytes, norm_workspace(M, d, batches));
+    kq::NormParams p{};
+    p.dy = dy;
+    p.dh = dh;
+    p.x = x;
+    p.h = const_cast<void*>(h);
+    p.gate = gate;
+    p.scale = scale;
+    p.gate_stride = gate_stride;
+    p.scale_stride = scale_stride;
+    p.weight = weight;
+    p.post_weight = post_weight;
+    p.M = M;
+    p.d = d;
+    p.rows = M / batches;
+    p.batches = batches;
+    p.chunks = kq::norm_chunks(M, batches, d);
+    p.norm = norm;
+    p.post = post_norm;
+    p.alpha = alpha;
+    p.eps = eps;
+    p.x16 = x_dtype == KQ_DTYPE_BF16;
+    p.stream16 = stream_dtype == KQ_DTYPE_BF16;
+    p.vec16 = vec_dtype == KQ_DTYPE_BF16;
+    p.dx = dx;
+    p.dresidual = dresidual;
+    p.dgate = dgate;
+    p.dscale = dscale;
+    p.dshift = dshift;
+    p.dweight = dweight;
+    p.dpost_weight = dpost_weight;
+    p.partial = static_cast<float*>(workspace);
+    return from_hip(kq::launch_block_norm_backward(p, (hipStream_t)stream), "kq_block_norm_backward");
 }
 
 kq_status kq_mxfp4_quantize(const uint16_t* X, int64_t M, int64_t d, uint8_t* codes, uint8_t* scales,

@@ -14,6 +14,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 
+#include <algorithm>
+
 #include "kroquant.h"
 
 namespace {
@@ -359,11 +361,273 @@ PyObject* calib_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+// fp32 or bf16, as the library's type.
+bool float_type(const at::Tensor* t, int* type) {
+    if (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16) return false;
+    *type = t->scalar_type() == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32;
+    return true;
+}
+
+bool number(PyObject* o, float* v) {
+    if (!PyFloat_CheckExact(o)) return false;
+    *v = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+bool small_int(PyObject* o, int* v) {
+    if (!PyLong_CheckExact(o)) return false;
+    *v = (int)PyLong_AsLong(o);
+    return true;
+}
+
+bool float_dtype(PyObject* o, at::ScalarType* t) {
+    if (!THPDtype_Check(o)) return false;
+    *t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+    return *t == at::kFloat || *t == at::kBFloat16;
+}
+
+// Vectors of one type, [d] or [B, d] with contiguous rows.
+struct Vectors {
+    int type = -1;
+    int64_t batches = -1;
+    at::Device dev;
+    explicit Vectors(at::Device d) : dev(d) {}
+    int dtype() const { return type < 0 ? KQ_DTYPE_FP32 : type; }
+    int64_t count() const { return batches < 0 ? 1 : batches; }
+    bool add(PyObject* o, int64_t d, bool per_batch, const void** p, int64_t* stride) {
+        *p = nullptr;
+        *stride = 0;
+        if (o == Py_None) return true;
+        const at::Tensor* t = tensor(o);
+        int ty;
+        if (!t || !t->is_cuda() || t->device() != dev || !float_type(t, &ty) || (type >= 0 && ty != type)) return false;
+        type = ty;
+        const int64_t dim = t->dim();
+        if (dim < 1 || dim > (per_batch ? 2 : 1) || t->size(dim - 1) != d || (d > 1 && t->stride(dim - 1) != 1)) return false;
+        if (per_batch) {
+            const int64_t n = dim == 2 ? t->size(0) : 1;
+            if (batches >= 0 && n != batches) return false;
+            batches = n;
+            if (dim == 2) *stride = t->stride(0);
+            if (*stride < 0) return false;
+        }
+        *p = t->data_ptr();
+        return true;
+    }
+};
+
+// A [rows, cols] array of the type `dtype` whose rows are contiguous: its row stride, -1 if it is none.
+int64_t row_stride(const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType dtype, at::Device dev) {
+    if (!t || !t->is_cuda() || t->scalar_type() != dtype || t->device() != dev || t->dim() != 2 || t->size(0) != rows ||
+        t->size(1) != cols || (cols > 1 && t->stride(1) != 1) || (rows > 1 && t->stride(0) < cols))
+        return -1;
+    return rows > 1 ? t->stride(0) : cols;
+}
+
+// The output of a linear layer: the caller's, or a new one of out_dtype (else `dtype`).
+bool linear_out(PyObject* given, PyObject* out_dtype, at::ScalarType dtype, int64_t rows, int64_t cols, at::Device dev, Out& out,
+                int64_t* ldo, at::ScalarType* type) {
+    *type = dtype;
+    if (given != Py_None) {
+        const at::Tensor* t = tensor(given);
+        if (!t || (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16)) return false;
+        *type = t->scalar_type();
+        *ldo = row_stride(t, rows, cols, *type, dev);
+        if (*ldo < 0) return false;
+        out.given = given;
+        out.ptr = t->data_ptr();
+        return true;
+    }
+    if (out_dtype != Py_None && !float_dtype(out_dtype, type)) return false;
+    out.made = empty({rows, cols}, *type, dev);
+    out.ptr = out.made.data_ptr();
+    *ldo = cols;
+    return true;
+}
+
+struct Operands {
+    const at::Tensor* t[4];
+    int64_t M, N, K, E = 1;
+    at::Device dev = at::kCPU;
+    bool parse(PyObject* const* v, bool experts) {
+        for (int i = 0; i < 4; ++i) {
+            t[i] = tensor(v[i]);
+            if (!dense(t[i], at::kByte) || t[i]->dim() != (experts && i >= 2 ? 3 : 2) || t[i]->device() != t[0]->device()) return false;
+        }
+        const int64_t b = experts ? 1 : 0;
+        M = t[0]->size(0);
+        K = 2 * t[0]->size(1);
+        N = t[2]->size(b);
+        if (experts) E = t[2]->size(0);
+        dev = t[0]->device();
+        return 2 * t[2]->size(b + 1) == K && t[1]->size(0) == M && t[1]->size(1) == K / 32 && t[3]->size(b) == N &&
+               t[3]->size(b + 1) == K / 32 && (!experts || t[3]->size(0) == E);
+    }
+    const uint8_t* p(int i) const { return static_cast<const uint8_t*>(t[i]->data_ptr()); }
+};
+
+// (a_codes, a_scales, b_codes, b_scales, bias, act, gate, residual, out, out_dtype, stream)
+PyObject* mxfp4_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Operands o;
+        int act;
+        void* st = nullptr;
+        if (!o.parse(v, false) || !small_int(v[5], &act) || !stream_of(v[10], &st)) return nullptr;
+        const int64_t cols = act == KQ_ACT_SWIGLU ? o.N / 2 : o.N;
+        if (act == KQ_ACT_SWIGLU && o.N % 2) return nullptr;
+        Vectors vec(o.dev);
+        const void *bias, *gate;
+        int64_t none, stride;
+        if (!vec.add(v[4], o.N, false, &bias, &none) || !vec.add(v[6], cols, true, &gate, &stride) || o.M % vec.count()) return nullptr;
+        at::ScalarType type = at::kBFloat16;
+        const at::Tensor* res = nullptr;
+        if (v[7] != Py_None) {
+            res = tensor(v[7]);
+            if (!res) return nullptr;
+            type = res->scalar_type();
+            if (type != at::kFloat && type != at::kBFloat16) return nullptr;
+        }
+        Out out;
+        int64_t ldo, ldr = 0;
+        if (!linear_out(v[8], v[9], type, o.M, cols, o.dev, out, &ldo, &type)) return nullptr;
+        if (res && (ldr = row_stride(res, o.M, cols, type, o.dev)) < 0) return nullptr;
+        if (!call("kq_mxfp4_linear", [&] {
+                return kq_mxfp4_linear(o.p(0), o.p(1), o.M, o.p(2), o.p(3), o.N, o.K, bias, gate, stride,
+                                       std::max<int64_t>(1, o.M / vec.count()), (kq_dtype)vec.dtype(), (kq_act)act,
+                                       res ? res->data_ptr() : nullptr, ldr, out.ptr, ldo,
+                                       type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, st);
+            }))
+            return nullptr;
+        return out.take();
+    });
+}
+
+// (a_codes, a_scales, b_codes, b_scales, offsets, rows, bias, act, row_scale, out, out_dtype, stream)
+PyObject* mxfp4_grouped_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 12) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Operands o;
+        int act;
+        void* st = nullptr;
+        if (!o.parse(v, true) || !small_int(v[7], &act) || !stream_of(v[11], &st)) return nullptr;
+        if (act == KQ_ACT_SWIGLU && o.N % 2) return nullptr;
+        const at::Tensor* off = tensor(v[4]);
+        if (!buffer(off, at::kInt, o.E + 1, o.dev)) return nullptr;
+        int64_t R = o.M;
+        const at::Tensor *rows = nullptr, *bias = nullptr, *scale = nullptr;
+        if (v[5] != Py_None) {
+            rows = tensor(v[5]);
+            if (!dense(rows, at::kInt) || rows->device() != o.dev) return nullptr;
+            R = rows->numel();
+        }
+        int vec = KQ_DTYPE_FP32;
+        if (v[6] != Py_None) {
+            bias = tensor(v[6]);
+            if (!bias || !float_type(bias, &vec) || !dense(bias, bias->scalar_type()) || bias->device() != o.dev ||
+                bias->dim() != 2 || bias->size(0) != o.E || bias->size(1) != o.N)
+                return nullptr;
+        }
+        if (v[8] != Py_None) {
+            scale = tensor(v[8]);
+            if (!buffer(scale, at::kFloat, R, o.dev)) return nullptr;
+        }
+        Out out;
+        int64_t ldo;
+        at::ScalarType type;
+        if (!linear_out(v[9], v[10], at::kBFloat16, R, act == KQ_ACT_SWIGLU ? o.N / 2 : o.N, o.dev, out, &ldo, &type)) return nullptr;
+        if (!call("kq_mxfp4_grouped_linear", [&] {
+                return kq_mxfp4_grouped_linear(o.p(0), o.p(1), o.M, rows ? static_cast<const int32_t*>(rows->data_ptr()) : nullptr,
+                                               R, o.p(2), o.p(3), o.E, o.N, o.K, static_cast<const int32_t*>(off->data_ptr()),
+                                               bias ? bias->data_ptr() : nullptr, (kq_dtype)vec, (kq_act)act,
+                                               scale ? static_cast<const float*>(scale->data_ptr()) : nullptr, out.ptr, ldo,
+                                               type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, st);
+            }))
+            return nullptr;
+        return out.take();
+    });
+}
+
+// A contiguous matrix as `like`, of one of the two types.
+const at::Tensor* as_matrix(PyObject* o, const at::Tensor* like, int* type) {
+    const at::Tensor* t = tensor(o);
+    if (!t || !t->is_cuda() || !t->is_contiguous() || t->dim() != 2 || !float_type(t, type)) return nullptr;
+    if (like && (t->size(0) != like->size(0) || t->size(1) != like->size(1) || t->device() != like->device())) return nullptr;
+    return t;
+}
+
+// The five vectors of a norm, from v[0]: gate, post_weight, weight, scale, shift.
+struct NormVectors {
+    const void *gate, *post_weight, *weight, *scale, *shift;
+    int64_t gs, ss, hs, none;
+    Vectors vec;
+    explicit NormVectors(at::Device dev) : vec(dev) {}
+    bool parse(PyObject* const* v, int64_t M, int64_t d) {
+        return vec.add(v[0], d, true, &gate, &gs) && vec.add(v[1], d, false, &post_weight, &none) &&
+               vec.add(v[2], d, false, &weight, &none) && vec.add(v[3], d, true, &scale, &ss) &&
+               vec.add(v[4], d, true, &shift, &hs) && vec.count() > 0 && M % vec.count() == 0;
+    }
+};
+
+// (x, residual, gate, post_weight, weight, scale, shift, norm, post_norm, alpha, eps, h, y, h_dtype, stream)
+PyObject* block_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 15) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        int xt, ht, norm, post;
+        float alpha, eps;
+        void* st = nullptr;
+        const at::Tensor* x = as_matrix(v[0], nullptr, &xt);
+        if (!x || !small_int(v[7], &norm) || !small_int(v[8], &post) || !number(v[9], &alpha) || !number(v[10], &eps) ||
+            !stream_of(v[14], &st) || norm == KQ_NORM_NONE)
+            return nullptr;
+        const int64_t M = x->size(0), d = x->size(1);
+        ht = xt;
+        const at::Tensor* res = nullptr;
+        if (v[1] != Py_None && !(res = as_matrix(v[1], x, &ht))) return nullptr;
+        if (!res && v[13] != Py_None) {
+            at::ScalarType t;
+            if (!float_dtype(v[13], &t)) return nullptr;
+            ht = t == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32;
+        }
+        NormVectors vs(x->device());
+        if (!vs.parse(v + 2, M, d)) return nullptr;
+        const bool plain = !res && !vs.gate && !post && alpha == 1.0f && ht == xt && v[11] == Py_None;
+        Out h, y;
+        const at::ScalarType hs = ht == KQ_DTYPE_BF16 ? at::kBFloat16 : at::kFloat;
+        if (v[11] != Py_None) {
+            int t;
+            if (!as_matrix(v[11], x, &t) || (res && t != ht)) return nullptr;
+            ht = t;
+            h.given = v[11];
+            h.ptr = tensor(v[11])->data_ptr();
+        } else if (!output(v[11], !plain, {M, d}, hs, M * d, x->device(), h)) {
+            return nullptr;
+        }
+        int yt = xt;
+        if (v[12] != Py_None && (!as_matrix(v[12], x, &yt) || yt != xt)) return nullptr;
+        if (!output(v[12], true, {M, d}, x->scalar_type(), M * d, x->device(), y)) return nullptr;
+        if (!call("kq_block_norm", [&] {
+                return kq_block_norm(x->data_ptr(), (kq_dtype)xt, res ? res->data_ptr() : nullptr, (kq_dtype)ht, M, d,
+                                     vs.vec.count(), vs.gate, vs.gs, vs.scale, vs.ss, vs.shift, vs.hs, vs.weight,
+                                     vs.post_weight, (kq_dtype)vs.vec.dtype(), (kq_norm)norm, (kq_norm)post, alpha, eps, h.ptr,
+                                     y.ptr, st);
+            }))
+            return nullptr;
+        if (plain) h.given = v[0];
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, h.take());
+        PyTuple_SET_ITEM(r, 1, y.take());
+        return r;
+    });
+}
+
 #define KQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {KQ_METHOD(quantize),    KQ_METHOD(quantize_exact), KQ_METHOD(quantize_packed),
                           KQ_METHOD(quantize_lu), KQ_METHOD(smoothquant),    KQ_METHOD(hadamard32),
                           KQ_METHOD(fwht),        KQ_METHOD(mxfp4),          KQ_METHOD(mxfp4_gemm),
-                          KQ_METHOD(calib_step),  {nullptr, nullptr, 0, nullptr}};
+                          KQ_METHOD(calib_step),  KQ_METHOD(mxfp4_linear),   KQ_METHOD(mxfp4_grouped_linear),
+                          KQ_METHOD(block_norm),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_kqbind", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,545 @@
+// W4A4 linear layers: the MXFP4 product with what follows it in its epilogue,
+//     out = residual + gate act(deq(A) deq(B)^T + bias),
+// and the same product grouped by expert, rows gathered and weighted,
+//     out[r] = row_scale[r] act(deq(A)[rows[r]] deq(B_e)^T + bias_e),
+// where expert e has the rows offsets[e] .. offsets[e + 1] - 1.  Products are
+// exact, sums and the epilogue are in 32 bits, out is rounded once.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kq_gemm_tile.h"
+#include "kq_linear.h"
+
+namespace kq {
+
+typedef float f32x4m __attribute__((ext_vector_type(4)));
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
+
+// act(p).  The exponentials and reciprocals are the hardware's (1 ulp each).
+template <Act A>
+__device__ __forceinline__ float activate(float p) {
+    if (A == Act::Relu) return fmaxf(p, 0.0f);
+    if (A == Act::Silu || A == Act::Swiglu) return p * sigmoid(p);
+    if (A == Act::GeluTanh) {
+        // p (1 + tanh z) / 2 = p sigmoid(2 z), z = sqrt(2 / pi) (p + 0.044715 p^3)
+        constexpr float c = -2.0f * kLog2e * 0.797884560802865356f;
+        return p * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(p * fmaf(c * 0.044715f, p * p, c)));
+    }
+    if (A == Act::Gelu) {
+        // p Phi(p), Phi(-a) = exp(-a^2 / 2) q(t) with t = 1 / (1 + 0.35 a): the polynomial q is a
+        // minimax fit of exp(a^2 / 2) Phi(-a) in relative error, 3.1e-7 for a <= 13.5 (Phi(-a) = 0 beyond)
+        const float a = fabsf(p), t = __builtin_amdgcn_rcpf(fmaf(0.35f, a, 1.0f));
+        float q = 0.048942483961582184f;
+        q = fmaf(q, t, -0.20211942493915558f);
+        q = fmaf(q, t, 0.2406410276889801f);
+        q = fmaf(q, t, -0.01702360063791275f);
+        q = fmaf(q, t, 0.1559615582227707f);
+        q = fmaf(q, t, 0.13335508108139038f);
+        q = fmaf(q, t, 0.14027033746242523f);
+        q = fmaf(q, t, -2.731548374867998e-05f);
+        q *= __builtin_amdgcn_exp2f(-0.5f * kLog2e * a * a);
+        const float m = a >= 13.5f ? 0.0f : p * q;
+        return p > 0.0f ? p - m : m;
+    }
+    return p;
+}
+
+// f with the call's activation as a compile-time constant.
+template <class F>
+__device__ __forceinline__ void with_act(Act a, F f) {
+    switch (a) {
+        case Act::None: f(std::integral_constant<Act, Act::None>{}); break;
+        case Act::Gelu: f(std::integral_constant<Act, Act::Gelu>{}); break;
+        case Act::GeluTanh: f(std::integral_constant<Act, Act::GeluTanh>{}); break;
+        case Act::Silu: f(std::integral_constant<Act, Act::Silu>{}); break;
+        case Act::Relu: f(std::integral_constant<Act, Act::Relu>{}); break;
+        case Act::Swiglu: f(std::integral_constant<Act, Act::Swiglu>{}); break;
+    }
+}
+
+__device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+// V (a multiple of 4) values of a bf16 or fp32 array from element `at`, the first `n` of them; zeros past.
+template <int V>
+__device__ __forceinline__ void load_values(const void* p, int is16, int64_t at, int n, float (&v)[V]) {
+    if (is16) {
+        const uint16_t* const q = static_cast<const uint16_t*>(p) + at;
+        if (n >= V) {
+#pragma unroll
+            for (int k = 0; k < V; k += 4) {
+                const u32x2b w = *reinterpret_cast<const u32x2b*>(q + k);
+                v[k] = __uint_as_float(w.x << 16);
+                v[k + 1] = __uint_as_float(w.x & 0xffff0000u);
+                v[k + 2] = __uint_as_float(w.y << 16);
+                v[k + 3] = __uint_as_float(w.y & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = k < n ? bf16_value(q[k]) : 0.f;
+        }
+    } else {
+        const float* const q = static_cast<const float*>(p) + at;
+        if (n >= V) {
+#pragma unroll
+            for (int k = 0; k < V; k += 4) {
+                const f32x4 w = *reinterpret_cast<const f32x4*>(q + k);
+                v[k] = w.x;
+                v[k + 1] = w.y;
+                v[k + 2] = w.z;
+                v[k + 3] = w.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = k < n ? q[k] : 0.f;
+        }
+    }
+}
+
+// The first n of V values to a bf16 or fp32 array.
+template <int V>
+__device__ __forceinline__ void store_values(void* p, int is16, int64_t at, int n, const float (&v)[V]) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if (is16) {
+        uint16_t* const q = static_cast<uint16_t*>(p) + at;
+        uint32_t w[V / 2];
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) w[k] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * k], (__bf16)v[2 * k + 1]});
+        if (n >= V) {
+            if constexpr (V == 8) *reinterpret_cast<u32x4b*>(q) = u32x4b{w[0], w[1], w[2], w[3]};
+            else if constexpr (V == 4) *reinterpret_cast<u32x2b*>(q) = u32x2b{w[0], w[1]};
+            else *reinterpret_cast<u32b*>(q) = w[0];
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k < n) q[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+        }
+    } else {
+        float* const q = static_cast<float*>(p) + at;
+        if (n >= V) {
+            typedef float f32x2 __attribute__((ext_vector_type(2), aligned(4)));
+            if constexpr (V == 2) *reinterpret_cast<f32x2*>(q) = f32x2{v[0], v[1]};
+            else
+#pragma unroll
+                for (int k = 0; k < V; k += 4) *reinterpret_cast<f32x4*>(q + k) = f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]};
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k < n) q[k] = v[k];
+        }
+    }
+}
+
+// V sums of row m from column n (v; `have` columns of them inside N) to the output: the epilogue where
+// everything is loaded as it is needed.
+template <Act A, int V>
+__device__ __forceinline__ void finish(const LinearParams& p, int64_t m, int64_t n, int have, float (&v)[V]) {
+    if (p.bias) {
+        float b[V];
+        load_values<V>(p.bias, p.vec16, n, have, b);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] += b[k];
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = A == Act::Swiglu && (k & 1) ? v[k] : activate<A>(v[k]);
+    const float rs = p.row_scale ? p.row_scale[m] : 1.0f;
+    constexpr int VO = A == Act::Swiglu ? V / 2 : V;
+    const int64_t c = A == Act::Swiglu ? n / 2 : n;
+    const int nc = A == Act::Swiglu ? have / 2 : have;
+    float o[VO];
+#pragma unroll
+    for (int k = 0; k < VO; ++k) o[k] = A == Act::Swiglu ? v[2 * k] * v[2 * k + 1] : v[k];
+    if (p.row_scale) {
+#pragma unroll
+        for (int k = 0; k < VO; ++k) o[k] *= rs;
+    }
+    if constexpr (VO >= 4) {
+        if (p.gate) {
+            float g[VO];
+            load_values<VO>(p.gate, p.vec16, m / p.gate_rows * p.gate_stride + c, nc, g);
+#pragma unroll
+            for (int k = 0; k < VO; ++k) o[k] *= g[k];
+        }
+        if (p.residual) {
+            float r[VO];
+            load_values<VO>(p.residual, p.out16, m * p.ldr + c, nc, r);
+#pragma unroll
+            for (int k = 0; k < VO; ++k) o[k] += r[k];
+        }
+    } else {
+        auto at = [&](const void* q, int is16, int64_t i) {
+            return is16 ? bf16_value(static_cast<const uint16_t*>(q)[i]) : static_cast<const float*>(q)[i];
+        };
+#pragma unroll
+        for (int k = 0; k < VO; ++k) {
+            if (k >= nc) break;
+            if (p.gate) o[k] *= at(p.gate, p.vec16, m / p.gate_rows * p.gate_stride + c + k);
+            if (p.residual) o[k] += at(p.residual, p.out16, m * p.ldr + c + k);
+        }
+    }
+    store_values<VO>(p.out, p.out16, m * p.ldo + c, nc, o);
+}
+
+// A grouped call's tile: which expert, and its place among the expert's row tiles.
+struct Group {
+    int expert;
+    int first, end;  // the expert's rows
+    int tile;        // row tile within it
+};
+
+// Row tiles of BM rows, the experts' one after the other; every lane of the wave calls it with the same
+// arguments.  Offsets outside [0, M] or decreasing are taken as an empty or a shorter group.
+struct GroupScan {
+    int cum, first, end;  // this lane's expert: tiles up to and with it, its rows
+    __device__ __forceinline__ void step(const LinearParams& p, int e0, int bm, int before) {
+        const int e = e0 + (threadIdx.x & 63), M = (int)p.g.M;
+        first = end = 0;
+        if (e < p.experts) {
+            first = min(max(p.offsets[e], 0), M);
+            end = min(max(p.offsets[e + 1], first), M);
+        }
+        int t = (end - first) / bm + ((end - first) % bm != 0);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(t, o);
+            if ((int)(threadIdx.x & 63) >= o) t += u;
+        }
+        cum = before + t;
+    }
+};
+__device__ __forceinline__ int64_t group_tiles(const LinearParams& p, int bm) {
+    int total = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {
+        GroupScan s;
+        s.step(p, e0, bm, total);
+        total = __builtin_amdgcn_readlane(s.cum, 63);
+    }
+    return total;
+}
+__device__ __forceinline__ Group find_group(const LinearParams& p, int bm, int tile) {
+    Group r{};
+    int before = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {
+        GroupScan s;
+        s.step(p, e0, bm, before);
+        const uint64_t past = __ballot(s.cum > tile);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            r.expert = e0 + l;
+            r.first = __builtin_amdgcn_readlane(s.first, l);
+            r.end = __builtin_amdgcn_readlane(s.end, l);
+            r.tile = tile - (l ? __builtin_amdgcn_readlane(s.cum, l - 1) : before);
+            return r;
+        }
+        before = __builtin_amdgcn_readlane(s.cum, 63);
+    }
+    return r;
+}
+
+// The tile of workgroup blockIdx.x: its place in C, and p narrowed to its expert.  False: none is left
+// (the host's grid is the most that any offsets can need).
+template <bool GROUPED>
+__device__ __forceinline__ bool place(LinearParams& p, int bn, int bm, int64_t& nb0, int64_t& mb0) {
+    const int64_t gx = (p.g.N + bn - 1) / bn;
+    int64_t gy = (p.g.M + bm - 1) / bm, tn, tm;
+    if (GROUPED) {
+        gy = group_tiles(p, bm);
+        if (blockIdx.x >= gx * gy) return false;
+    }
+    xcd_tile(gx, gy, tn, tm);
+    nb0 = tn * bn;
+    mb0 = tm * bm;
+    if (GROUPED) {
+        const Group r = find_group(p, bm, (int)tm);
+        if (r.first >= r.end) return false;
+        mb0 = r.first + (int64_t)r.tile * bm;
+        p.g.M = r.end;
+        p.g.b_codes += r.expert * p.g.N * (p.g.K / 2);
+        p.g.b_scales += r.expert * p.g.N * (p.g.K / 32);
+        if (p.bias) p.bias = static_cast<const uint8_t*>(p.bias) + r.expert * p.g.N * (p.vec16 ? 2 : 4);
+    }
+    return true;
+}
+
+}  // namespace
+
+// The pipelined tile's sums to the output, through LDS in fp32 so that the output and the residual are
+// accessed along their rows.  A thread keeps its eight columns: bias and gate are loaded once (the gate
+// again at another batch's rows).
+// RES: the residual's loads of a pass are issued before its stores (a wait for a load waits for every
+// store issued before it too).
+template <int WN, int WM, int TN, int TM, bool RES>
+__device__ __forceinline__ void finish_tile(const LinearParams& p, uint8_t* lds, int64_t nb0, int64_t mb0,
+                                            const f32x16g (&acc)[TN][TM]) {
+    typedef Tile<WN, WM, TN, TM> T;
+    constexpr int NP = (T::BM * (T::BN * 4 + 16) <= (int)sizeof(typename T::Lds)) ? 1 : 2;
+    constexpr int TP = TN / NP, RB = T::BN / NP * 4, RS = RB + 16;
+    static_assert(T::BM * RS <= (int)sizeof(typename T::Lds), "a pass fits LDS");
+    constexpr int V = 8, CPR = RB / (4 * V), STEP = 64 * T::WAVES / CPR, CH = T::BM / STEP;
+    static_assert(32 * TP % V == 0 && 64 * T::WAVES % CPR == 0, "a thread keeps its columns, inside one wave's range");
+    const int t = threadIdx.x;
+    const int wave = t >> 6, lane = t & 63;
+    const int r = lane & 31, h = lane >> 5, wn = wave / WM, wm = wave % WM;
+    const int last = (int)min<int64_t>(T::BM, p.g.M - mb0) - 1;
+    const int trow = t / CPR, cl = t % CPR * V, seg = cl / (32 * TP);
+    const bool glu = p.act == Act::Swiglu;
+#pragma unroll
+    for (int pass = 0; pass < NP; ++pass) {
+        const int64_t n = nb0 + seg * 32 * TN + 32 * pass * TP + (cl - seg * 32 * TP);
+        const int have = (int)max<int64_t>(0, min<int64_t>(V, p.g.N - n));
+        if (pass > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                uint8_t* const dst = lds + (32 * (wm * TM + j) + r) * RS + (32 * (wn * TP + i) + 4 * h) * 4;
+                const f32x16g& c = acc[pass * TP + i][j];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4*>(dst + 32 * q) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
+            }
+        __builtin_amdgcn_sched_barrier(0);  // the pass's accumulators are free for what is loaded
+        float bias[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) bias[k] = 0.f;
+        if (p.bias && have > 0) load_values<V>(p.bias, p.vec16, n, have, bias);
+        __syncthreads();
+        const uint8_t* const from = lds + trow * RS + 4 * cl;
+        if (have > 0) {
+            with_act(p.act, [&](auto act) {
+                constexpr Act A = decltype(act)::value;
+#pragma unroll 2
+                for (int k = 0; k < CH; ++k) {
+                    if (trow + k * STEP > last) break;
+                    const float4 a = *reinterpret_cast<const float4*>(from + k * STEP * RS);
+                    const float4 b = *reinterpret_cast<const float4*>(from + k * STEP * RS + 16);
+                    float v[V] = {a.x + bias[0], a.y + bias[1], a.z + bias[2], a.w + bias[3],
+                                  b.x + bias[4], b.y + bias[5], b.z + bias[6], b.w + bias[7]};
+                    LinearParams q = p;
+                    q.bias = nullptr;
+                    finish<A, V>(q, mb0 + trow + k * STEP, n, have, v);
+                }
+            });
+        }
+    }
+    (void)glu;
+}
+
+template <int WN, int WM, int TN, int TM, bool PING, bool DMA_SCALES, bool GROUPED, bool GATHER>
+__global__ __launch_bounds__(64 * WN * WM) void mxfp4_linear_pipe_kernel(LinearParams p) {
+    typedef Tile<WN, WM, TN, TM> T;
+    __shared__ typename T::Lds lds;
+    int64_t nb0, mb0;
+    if (!place<GROUPED>(p, T::BN, T::BM, nb0, mb0)) return;
+    f32x16g acc[TN][TM];
+    gemm_tile<WN, WM, TN, TM, PING, DMA_SCALES, GATHER>(p.g, lds, nb0, mb0, acc);
+    finish_tile<WN, WM, TN, TM, false>(p, reinterpret_cast<uint8_t*>(&lds), nb0, mb0, acc);
+}
+
+// Few tiles of more than a few rows: W waves share a tile and split K.
+template <int TN, int TM, int W, int D, bool GROUPED, bool GATHER>
+__global__ __launch_bounds__(64 * W) void mxfp4_linear_split_kernel(LinearParams p) {
+    constexpr int BN = 32 * TN, BM = 32 * TM, RS = BN + 4;
+    __shared__ float sums[W * BM * RS];
+    int64_t nb0, mb0;
+    if (!place<GROUPED>(p, BN, BM, nb0, mb0)) return;
+    const int active = split_tile<TN, TM, W, D, GATHER>(p.g, sums, nb0, mb0);
+    with_act(p.act, [&](auto act) {
+        for (int k = threadIdx.x; k < BM * BN / 4; k += 64 * W) {
+            const int row = k / (BN / 4), col = 4 * (k % (BN / 4));
+            const int64_t m = mb0 + row, n = nb0 + col;
+            if (m >= p.g.M || n >= p.g.N) continue;
+            float4 s = *reinterpret_cast<const float4*>(sums + row * RS + col);
+            for (int w = 1; w < active; ++w) {
+                const float4 o = *reinterpret_cast<const float4*>(sums + (w * BM + row) * RS + col);
+                s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+            }
+            float v[4] = {s.x, s.y, s.z, s.w};
+            finish<decltype(act)::value, 4>(p, m, n, (int)min<int64_t>(4, p.g.N - n), v);
+        }
+    });
+}
+
+// A few rows (a decoding step): the weight is read once and bounds the call.  A tile is 16 TM rows of A
+// by 16 of B; v_mfma_scale_f32_16x16x128_f8f6f4 takes lane l's 16 code bytes as row l % 16, block l / 16
+// of the 128-wide K step, so fragments are plain loads.  WN waves have a tile each, next to each other
+// along N, and WK waves split each tile's K, in units of 256 (whole 128-byte lines of B), D units in flight;
+// their sums meet in LDS in wave order.
+template <int TM, int WN, int WK, int D, bool GROUPED, bool GATHER>
+__global__ __launch_bounds__(64 * WN * WK) void mxfp4_linear_rows_kernel(LinearParams p) {
+    constexpr int BM = 16 * TM, BN = 16 * WN, RS = 20;  // LDS row in floats
+    __shared__ float sums[WN * WK * BM * RS];
+    int64_t nb0, mb0;
+    if (!place<GROUPED>(p, BN, BM, nb0, mb0)) return;
+    const GemmParams& g = p.g;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wn = wave / WK, wk = wave % WK, r = lane & 15, b = lane >> 4;
+    const int64_t nkb = g.K / 32, row_bytes = g.K / 2, units = (nkb + 7) / 8;
+    const int64_t nrow = min(nb0 + 16 * wn + r, g.N - 1);  // rows past N or M read the last row
+    const uint8_t *cw = g.b_codes + nrow * row_bytes, *sw = g.b_scales + nrow * nkb, *cx[TM], *sx[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        int64_t m = min(mb0 + 16 * j + r, g.M - 1);
+        if (GATHER) m = gathered(g, m);
+        cx[j] = g.a_codes + m * row_bytes;
+        sx[j] = g.a_scales + m * nkb;
+    }
+    struct Unit {
+        uint4 w[2], x[2][TM];
+        uint32_t sw[2], sx[2][TM];
+    };
+    auto load = [&](int64_t u, Unit& f) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int64_t k = min(8 * u + 4 * s + b, nkb - 1);  // blocks past K read the last one; masked below
+            f.w[s] = *reinterpret_cast<const uint4*>(cw + 16 * k);
+            f.sw[s] = sw[k];
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                f.x[s][j] = *reinterpret_cast<const uint4*>(cx[j] + 16 * k);
+                f.sx[s][j] = sx[j][k];
+            }
+        }
+    };
+    f32x4m acc[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[j] = f32x4m{};
+    auto multiply = [&](int64_t u, Unit& f) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (8 * u + 4 * s + b >= nkb) {  // zero codes, scale 1
+                f.w[s] = make_uint4(0u, 0u, 0u, 0u);
+                f.sw[s] = 127u;
+#pragma unroll
+                for (int j = 0; j < TM; ++j) f.sx[s][j] = 127u;
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+                acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(Frag{f.w[s], 0u}), operand(Frag{f.x[s][j], 0u}),
+                                                                          acc[j], 4, 4, 0, (int)f.sw[s], 0, (int)f.sx[s][j]);
+        }
+    };
+    Unit f[D];
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+        if (wk + i * WK < units) load(wk + i * WK, f[i]);
+    for (int64_t u = wk; u < units; u += D * WK) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int64_t v = u + i * WK;
+            if (v < units) {
+                multiply(v, f[i]);
+                if (v + D * WK < units) load(v + D * WK, f[i]);
+            }
+        }
+    }
+    // acc[j][e]: row 16 j + r of A, row 4 b + e of B
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+        *reinterpret_cast<float4*>(sums + ((wn * WK + wk) * BM + 16 * j + r) * RS + 4 * b) =
+            make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+    __syncthreads();
+    with_act(p.act, [&](auto act) {
+        for (int k = threadIdx.x; k < WN * BM * 4; k += 64 * WN * WK) {
+            const int c = k % (4 * WN), row = k / (4 * WN);
+            const int64_t m = mb0 + row, n = nb0 + 4 * c;
+            if (m >= g.M || n >= g.N) continue;
+            const float* const from = sums + (c / 4 * WK * BM + row) * RS + 4 * (c % 4);
+            float4 s = *reinterpret_cast<const float4*>(from);
+#pragma unroll
+            for (int w = 1; w < WK; ++w) {
+                const float4 o = *reinterpret_cast<const float4*>(from + w * BM * RS);
+                s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+            }
+            float v[4] = {s.x, s.y, s.z, s.w};
+            finish<decltype(act)::value, 4>(p, m, n, (int)min<int64_t>(4, g.N - n), v);
+        }
+    });
+}
+
+constexpr int64_t kPipeMaxK = int64_t(1) << 24;  // 32-bit offsets within a tile
+
+// Row tiles that a call can need: every group may end inside one.
+static int64_t row_tiles(const LinearParams& p, int64_t bm) {
+    if (!p.offsets) return (p.g.M + bm - 1) / bm;
+    return p.g.M / bm + std::min(p.experts, p.g.M);
+}
+
+enum class LinearTile { Rows16, Rows32, Rows64, Split32, Split64, Pipe128, Pipe256 };
+
+static LinearTile linear_tile_of(const LinearParams& p) {
+    const GemmParams& g = p.g;
+    auto tiles = [&](int64_t tm, int64_t tn) { return row_tiles(p, tm) * ((g.N + tn - 1) / tn); };
+    // rows that share a weight: those of the average group
+    const int64_t rows = p.offsets ? (g.M + p.experts - 1) / p.experts : g.M;
+    if (rows <= 16) return LinearTile::Rows16;
+    if (rows <= 32) return LinearTile::Rows32;
+    if (rows <= 64) return LinearTile::Rows64;
+    // gathered pipelined tiles have 32-bit offsets into all of A
+    const bool pipe = g.K <= kPipeMaxK && (!g.rows || g.a_rows <= (int64_t(1) << 32) / (g.K / 2));
+    if (tiles(32, 32) <= 256) return LinearTile::Split32;
+    if (tiles(64, 64) <= 256 || !pipe) return LinearTile::Split64;
+    const int64_t rounds128 = (tiles(128, 128) + 511) / 512, rounds256 = (tiles(256, 256) + 255) / 256;
+    if (g.K <= 1536 && rounds128 < 2 * rounds256) return LinearTile::Pipe128;
+    return g.K <= 128 || rounds128 <= rounds256 ? LinearTile::Pipe128 : LinearTile::Pipe256;
+}
+
+// Calls f(std::integral_constant<bool, GROUPED>, std::integral_constant<bool, GATHER>).
+template <class F>
+static void by_group(const LinearParams& p, F f) {
+    if (!p.offsets) f(std::false_type{}, std::false_type{});
+    else if (!p.g.rows) f(std::true_type{}, std::false_type{});
+    else f(std::true_type{}, std::true_type{});
+}
+
+template <int TM, int WN, int WK, int D>
+static void launch_rows(const LinearParams& p, hipStream_t st) {
+    const dim3 grid((unsigned)((p.g.N + 16 * WN - 1) / (16 * WN) * row_tiles(p, 16 * TM)));
+    by_group(p, [&](auto grouped, auto gather) {
+        hipLaunchKernelGGL((mxfp4_linear_rows_kernel<TM, WN, WK, D, decltype(grouped)::value, decltype(gather)::value>), grid,
+                           dim3(64 * WN * WK), 0, st, p);
+    });
+}
+
+template <int TN, int TM, int W, int D>
+static void launch_split(const LinearParams& p, hipStream_t st) {
+    const dim3 grid((unsigned)((p.g.N + 32 * TN - 1) / (32 * TN) * row_tiles(p, 32 * TM)));
+    by_group(p, [&](auto grouped, auto gather) {
+        hipLaunchKernelGGL((mxfp4_linear_split_kernel<TN, TM, W, D, decltype(grouped)::value, decltype(gather)::value>), grid,
+                           dim3(64 * W), 0, st, p);
+    });
+}
+
+template <int WN, int WM, int TN, int TM, bool PING>
+static void launch_pipe(const LinearParams& p, hipStream_t st) {
+    typedef Tile<WN, WM, TN, TM> T;
+    const dim3 grid((unsigned)((p.g.N + T::BN - 1) / T::BN * row_tiles(p, T::BM)));
+    const int64_t nkb = p.g.K / 32;
+    const bool dma = nkb % 4 == 0 && nkb >= 16 && p.g.scales_aligned;
+    by_group(p, [&](auto grouped, auto gather) {
+        constexpr bool GR = decltype(grouped)::value, GA = decltype(gather)::value;
+        if (dma) hipLaunchKernelGGL((mxfp4_linear_pipe_kernel<WN, WM, TN, TM, PING, true, GR, GA>), grid, dim3(64 * T::WAVES), 0, st, p);
+        else hipLaunchKernelGGL((mxfp4_linear_pipe_kernel<WN, WM, TN, TM, PING, false, GR, GA>), grid, dim3(64 * T::WAVES), 0, st, p);
+    });
+}
+
+int64_t mxfp4_grouped_workgroups(const LinearParams& p) { return (p.g.N + 15) / 16 * row_tiles(p, 16); }
+
+hipError_t launch_mxfp4_linear(const LinearParams& p, hipStream_t st) {
+    switch (linear_tile_of(p)) {
+        case LinearTile::Rows16: launch_rows<1, 1, 8, 3>(p, st); break;
+        case LinearTile::Rows32: launch_rows<2, 1, 8, 3>(p, st); break;
+        case LinearTile::Rows64: launch_rows<4, 1, 8, 2>(p, st); break;
+        case LinearTile::Split32: launch_split<1, 1, 8, 4>(p, st); break;
+        case LinearTile::Split64: launch_split<2, 2, 8, 2>(p, st); break;
+        case LinearTile::Pipe128: launch_pipe<2, 2, 2, 2, false>(p, st); break;
+        case LinearTile::Pipe256: launch_pipe<2, 4, 4, 2, true>(p, st); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace kq
