@@ -513,6 +513,7 @@ kq_status kq_block_norm(const void* x, kq_dtype x_dtype, const void* residual, k
     p.M = M;
     p.d = d;
     p.rows = M / batches;
+    p.batches = batches;
     p.norm = norm;
     p.post = post_norm;
     p.alpha = alpha;
@@ -578,7 +579,6 @@ kq_status kq_block_norm_backward(const void* dy, const void* dh, const void* x, 
     p.d = d;
     p.rows = M / batches;
     p.batches = batches;
-    p.chunks = kq::norm_chunks(M, batches, d);
     p.norm = norm;
     p.post = post_norm;
     p.alpha = alpha;

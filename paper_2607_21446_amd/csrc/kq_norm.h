@@ -32,12 +32,16 @@ struct NormParams {
     float *dgate, *dscale, *dshift;  // [B, d] or null
     float *dweight, *dpost_weight;   // [d] or null
     float* partial;         // [B, chunks, 3, d]
-    int64_t batches, chunks;
+    int64_t batches;
+    // filled in by the launcher: workgroups of a batch; waves that share a row and rows that a workgroup
+    // works on at once
+    int64_t chunks;
+    int waves, teams;
 };
 
-// Row chunks of a batch in the backward pass: one workgroup and one set of partial sums each.
+// Workgroups of a batch in the backward pass, each with its partial sums.
 int64_t norm_chunks(int64_t M, int64_t batches, int64_t d);
-hipError_t launch_block_norm(const NormParams& p, hipStream_t st);
-hipError_t launch_block_norm_backward(const NormParams& p, hipStream_t st);
+hipError_t launch_block_norm(NormParams p, hipStream_t st);
+hipError_t launch_block_norm_backward(NormParams p, hipStream_t st);
 
 }  // namespace kq
