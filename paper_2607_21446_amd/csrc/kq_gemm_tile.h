@@ -39,6 +39,16 @@ typedef uint32_t u32b __attribute__((aligned(2)));
 typedef uint32_t u32x2b __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4b __attribute__((ext_vector_type(4), aligned(2)));
 
+// A value that is the same in all lanes, in scalar registers: the compiler's own choice may be vector ones, which
+// the loads into LDS do not take as their base.
+template <class T>
+__device__ __forceinline__ T scalar(T v) {
+    static_assert(sizeof(T) == 8, "two registers");
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+    return __builtin_bit_cast(T, ((uint64_t)hi << 32) | lo);
+}
+
 // The row of a_codes that row m of X is (any index is kept inside the array).
 __device__ __forceinline__ int64_t gathered(const GemmParams& g, int64_t m) {
     return min(max((int64_t)g.rows[m], (int64_t)0), g.a_rows - 1);
@@ -160,8 +170,8 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& g, typename Tile<WN,
     const int last = (int)min<int64_t>(63, max<int64_t>(0, rows - 1 - row0));  // last row of the 64 to read
     const bool gather = GATHER && !isw;
     const int64_t rowc = min(row0, rows - 1), row1 = gather ? 0 : rowc;
-    const uint8_t* const cbase = (isw ? g.b_codes : g.a_codes) + row1 * row_bytes;
-    const uint8_t* const sbase = (isw ? g.b_scales : g.a_scales) + row1 * nkb;
+    const uint8_t* const cbase = scalar((isw ? g.b_codes : g.a_codes) + row1 * row_bytes);
+    const uint8_t* const sbase = scalar((isw ? g.b_scales : g.a_scales) + row1 * nkb);
     const int q = lane >> 2, blk = (lane & 3) ^ ((q >> 2) & 3);
     auto offset = [&](int i) { return gather ? (uint32_t)gathered(g, rowc + min(i, last)) : (uint32_t)min(i, last); };
     uint32_t voff[4];

@@ -12,6 +12,9 @@
 
 namespace kq {
 
+// Lambdas over the parameters: one that is called keeps them in scratch memory.
+#define KQ_INLINE __attribute__((always_inline))
+
 typedef float f32x4m __attribute__((ext_vector_type(4)));
 
 namespace {
@@ -267,12 +270,41 @@ __device__ __forceinline__ bool place(LinearParams& p, int bn, int bm, int64_t& 
 
 }  // namespace
 
+// V values of a bf16 or fp32 array as they are stored (bf16: the first V / 2 words).
+template <int V>
+__device__ __forceinline__ void load_stored(const void* p, int is16, int64_t at, uint32_t (&w)[V]) {
+    typedef uint32_t u32x4f __attribute__((ext_vector_type(4), aligned(4)));
+    if (is16) {
+        const uint16_t* const q = static_cast<const uint16_t*>(p) + at;
+        if constexpr (V == 8) {
+            const u32x4b v = *reinterpret_cast<const u32x4b*>(q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = v[k];
+        } else {
+            const u32x2b v = *reinterpret_cast<const u32x2b*>(q);
+            w[0] = v.x;
+            w[1] = v.y;
+        }
+    } else {
+        const uint32_t* const q = static_cast<const uint32_t*>(p) + at;
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const u32x4f v = *reinterpret_cast<const u32x4f*>(q + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[k + e] = v[e];
+        }
+    }
+}
+template <int V>
+__device__ __forceinline__ float stored_value(const uint32_t (&w)[V], int is16, int k) {
+    return __uint_as_float(!is16 ? w[k] : k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+}
+
 // The pipelined tile's sums to the output, through LDS in fp32 so that the output and the residual are
-// accessed along their rows.  A thread keeps its eight columns: bias and gate are loaded once (the gate
-// again at another batch's rows).
-// RES: the residual's loads of a pass are issued before its stores (a wait for a load waits for every
-// store issued before it too).
-template <int WN, int WM, int TN, int TM, bool RES>
+// accessed along their rows.  A thread keeps its eight columns: the bias is loaded once a pass, and the gate
+// where the tile's rows are of one batch.  The residual's and the router's loads of a pass are issued before its
+// stores (a wait for a load waits for every store issued before it too).
+template <int WN, int WM, int TN, int TM, bool GROUPED>
 __device__ __forceinline__ void finish_tile(const LinearParams& p, uint8_t* lds, int64_t nb0, int64_t mb0,
                                             const f32x16g (&acc)[TN][TM]) {
     typedef Tile<WN, WM, TN, TM> T;
@@ -286,9 +318,9 @@ __device__ __forceinline__ void finish_tile(const LinearParams& p, uint8_t* lds,
     const int r = lane & 31, h = lane >> 5, wn = wave / WM, wm = wave % WM;
     const int last = (int)min<int64_t>(T::BM, p.g.M - mb0) - 1;
     const int trow = t / CPR, cl = t % CPR * V, seg = cl / (32 * TP);
-    const bool glu = p.act == Act::Swiglu;
-#pragma unroll
-    for (int pass = 0; pass < NP; ++pass) {
+    const bool one_gate = !GROUPED && p.gate && mb0 / p.gate_rows == (mb0 + last) / p.gate_rows;
+    auto one_pass = [&](auto which) KQ_INLINE {
+        constexpr int pass = decltype(which)::value;
         const int64_t n = nb0 + seg * 32 * TN + 32 * pass * TP + (cl - seg * 32 * TP);
         const int have = (int)max<int64_t>(0, min<int64_t>(V, p.g.N - n));
         if (pass > 0) __syncthreads();
@@ -303,30 +335,75 @@ __device__ __forceinline__ void finish_tile(const LinearParams& p, uint8_t* lds,
                     *reinterpret_cast<float4*>(dst + 32 * q) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
             }
         __builtin_amdgcn_sched_barrier(0);  // the pass's accumulators are free for what is loaded
-        float bias[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) bias[k] = 0.f;
-        if (p.bias && have > 0) load_values<V>(p.bias, p.vec16, n, have, bias);
-        __syncthreads();
         const uint8_t* const from = lds + trow * RS + 4 * cl;
-        if (have > 0) {
-            with_act(p.act, [&](auto act) {
-                constexpr Act A = decltype(act)::value;
-#pragma unroll 2
-                for (int k = 0; k < CH; ++k) {
-                    if (trow + k * STEP > last) break;
-                    const float4 a = *reinterpret_cast<const float4*>(from + k * STEP * RS);
-                    const float4 b = *reinterpret_cast<const float4*>(from + k * STEP * RS + 16);
-                    float v[V] = {a.x + bias[0], a.y + bias[1], a.z + bias[2], a.w + bias[3],
-                                  b.x + bias[4], b.y + bias[5], b.z + bias[6], b.w + bias[7]};
-                    LinearParams q = p;
-                    q.bias = nullptr;
-                    finish<A, V>(q, mb0 + trow + k * STEP, n, have, v);
+        with_act(p.act, [&](auto act) KQ_INLINE {
+            constexpr Act A = decltype(act)::value;
+            constexpr int VO = A == Act::Swiglu ? V / 2 : V;
+            const int64_t c = A == Act::Swiglu ? n / 2 : n;
+            float bias[V], gate[VO], scale[GROUPED ? CH : 1];
+            uint32_t res[GROUPED ? 1 : CH][VO];
+#pragma unroll
+            for (int k = 0; k < V; ++k) bias[k] = 0.f;
+            if (have == V) {
+                if (p.bias) load_values<V>(p.bias, p.vec16, n, V, bias);
+                if (GROUPED) {
+                    if (p.row_scale) {
+#pragma unroll
+                        for (int k = 0; k < CH; ++k) scale[GROUPED ? k : 0] = p.row_scale[mb0 + min(trow + k * STEP, last)];
+                    }
+                } else {
+                    if (one_gate) load_values<VO>(p.gate, p.vec16, mb0 / p.gate_rows * p.gate_stride + c, VO, gate);
+                    if (p.residual) {  // rows past M load the last one again
+#pragma unroll
+                        for (int k = 0; k < CH; ++k)
+                            load_stored<VO>(p.residual, p.out16, (mb0 + min(trow + k * STEP, last)) * p.ldr + c, res[GROUPED ? 0 : k]);
+                    }
                 }
-            });
-        }
-    }
-    (void)glu;
+            }
+            __syncthreads();
+            if (have < V) {
+                if (have > 0)
+                    for (int k = 0; k < CH && trow + k * STEP <= last; ++k) {
+                        float v[V];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[e] = reinterpret_cast<const float*>(from + k * STEP * RS)[e];
+                        finish<A, V>(p, mb0 + trow + k * STEP, n, have, v);
+                    }
+                return;
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                if (trow + k * STEP > last) break;
+                const int64_t m = mb0 + trow + k * STEP;
+                const float4 a = *reinterpret_cast<const float4*>(from + k * STEP * RS);
+                const float4 b = *reinterpret_cast<const float4*>(from + k * STEP * RS + 16);
+                const float v[V] = {a.x + bias[0], a.y + bias[1], a.z + bias[2], a.w + bias[3],
+                                    b.x + bias[4], b.y + bias[5], b.z + bias[6], b.w + bias[7]};
+                float o[VO];
+#pragma unroll
+                for (int e = 0; e < VO; ++e) o[e] = A == Act::Swiglu ? activate<A>(v[2 * e]) * v[2 * e + 1] : activate<A>(v[e]);
+                if (GROUPED) {
+                    if (p.row_scale) {
+#pragma unroll
+                        for (int e = 0; e < VO; ++e) o[e] *= scale[GROUPED ? k : 0];
+                    }
+                } else {
+                    if (p.gate) {
+                        if (!one_gate) load_values<VO>(p.gate, p.vec16, m / p.gate_rows * p.gate_stride + c, VO, gate);
+#pragma unroll
+                        for (int e = 0; e < VO; ++e) o[e] *= gate[e];
+                    }
+                    if (p.residual) {
+#pragma unroll
+                        for (int e = 0; e < VO; ++e) o[e] += stored_value<VO>(res[GROUPED ? 0 : k], p.out16, e);
+                    }
+                }
+                store_values<VO>(p.out, p.out16, m * p.ldo + c, VO, o);
+            }
+        });
+    };
+    one_pass(std::integral_constant<int, 0>{});
+    if constexpr (NP > 1) one_pass(std::integral_constant<int, 1>{});
 }
 
 template <int WN, int WM, int TN, int TM, bool PING, bool DMA_SCALES, bool GROUPED, bool GATHER>
@@ -337,7 +414,7 @@ __global__ __launch_bounds__(64 * WN * WM) void mxfp4_linear_pipe_kernel(LinearP
     if (!place<GROUPED>(p, T::BN, T::BM, nb0, mb0)) return;
     f32x16g acc[TN][TM];
     gemm_tile<WN, WM, TN, TM, PING, DMA_SCALES, GATHER>(p.g, lds, nb0, mb0, acc);
-    finish_tile<WN, WM, TN, TM, false>(p, reinterpret_cast<uint8_t*>(&lds), nb0, mb0, acc);
+    finish_tile<WN, WM, TN, TM, GROUPED>(p, reinterpret_cast<uint8_t*>(&lds), nb0, mb0, acc);
 }
 
 // Few tiles of more than a few rows: W waves share a tile and split K.
@@ -348,7 +425,7 @@ __global__ __launch_bounds__(64 * W) void mxfp4_linear_split_kernel(LinearParams
     int64_t nb0, mb0;
     if (!place<GROUPED>(p, BN, BM, nb0, mb0)) return;
     const int active = split_tile<TN, TM, W, D, GATHER>(p.g, sums, nb0, mb0);
-    with_act(p.act, [&](auto act) {
+    with_act(p.act, [&](auto act) KQ_INLINE {
         for (int k = threadIdx.x; k < BM * BN / 4; k += 64 * W) {
             const int row = k / (BN / 4), col = 4 * (k % (BN / 4));
             const int64_t m = mb0 + row, n = nb0 + col;
@@ -443,7 +520,7 @@ __global__ __launch_bounds__(64 * WN * WK) void mxfp4_linear_rows_kernel(LinearP
         *reinterpret_cast<float4*>(sums + ((wn * WK + wk) * BM + 16 * j + r) * RS + 4 * b) =
             make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
     __syncthreads();
-    with_act(p.act, [&](auto act) {
+    with_act(p.act, [&](auto act) KQ_INLINE {
         for (int k = threadIdx.x; k < WN * BM * 4; k += 64 * WN * WK) {
             const int c = k % (4 * WN), row = k / (4 * WN);
             const int64_t m = mb0 + row, n = nb0 + 4 * c;
