@@ -423,6 +423,8 @@ kq_status kq_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64
     if (!aligned(gate, dtype_bytes(vec_dtype)) || !aligned(residual, dtype_bytes(out_dtype)))
         return fail(KQ_ERROR_MISALIGNED, "gate and residual must be aligned to their elements");
     if (M == 0 || N == 0) return ok();
+    if (((M + 63) / 64) * ((N + 63) / 64) > INT32_MAX)
+        return fail(KQ_ERROR_UNSUPPORTED, "M = %lld and N = %lld need more workgroups than one launch holds", (long long)M, (long long)N);
     kq::LinearParams p = linear_params(a_codes, a_scales, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
     p.gate = gate;
     p.gate_stride = gate_stride;

@@ -27,9 +27,10 @@ struct LinearParams {
     // grouped: rows offsets[e] .. offsets[e + 1] - 1 take expert e's weight, b_codes + e N K / 2
     const int32_t* offsets = nullptr;
     int64_t experts = 0;
+    int stream_out = 0;  // filled in by the launcher: the output is stored past the caches
 };
 
-hipError_t launch_mxfp4_linear(const LinearParams& p, hipStream_t st);
+hipError_t launch_mxfp4_linear(LinearParams p, hipStream_t st);
 // Workgroups of a grouped call's largest launch, against the grid limit.
 int64_t mxfp4_grouped_workgroups(const LinearParams& p);
 

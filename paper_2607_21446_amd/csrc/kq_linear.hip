@@ -103,8 +103,15 @@ __device__ __forceinline__ void load_values(const void* p, int is16, int64_t at,
     }
 }
 
+// *q = v; PAST: past the caches, which would not keep it.
+template <bool PAST, class T>
+__device__ __forceinline__ void put(T* q, T v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, q);
+    else *q = v;
+}
+
 // The first n of V values to a bf16 or fp32 array.
-template <int V>
+template <int V, bool PAST = false>
 __device__ __forceinline__ void store_values(void* p, int is16, int64_t at, int n, const float (&v)[V]) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     if (is16) {
@@ -113,8 +120,8 @@ __device__ __forceinline__ void store_values(void* p, int is16, int64_t at, int 
 #pragma unroll
         for (int k = 0; k < V / 2; ++k) w[k] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * k], (__bf16)v[2 * k + 1]});
         if (n >= V) {
-            if constexpr (V == 8) *reinterpret_cast<u32x4b*>(q) = u32x4b{w[0], w[1], w[2], w[3]};
-            else if constexpr (V == 4) *reinterpret_cast<u32x2b*>(q) = u32x2b{w[0], w[1]};
+            if constexpr (V == 8) put<PAST>(reinterpret_cast<u32x4b*>(q), u32x4b{w[0], w[1], w[2], w[3]});
+            else if constexpr (V == 4) put<PAST>(reinterpret_cast<u32x2b*>(q), u32x2b{w[0], w[1]});
             else *reinterpret_cast<u32b*>(q) = w[0];
         } else {
 #pragma unroll
@@ -128,7 +135,7 @@ __device__ __forceinline__ void store_values(void* p, int is16, int64_t at, int 
             if constexpr (V == 2) *reinterpret_cast<f32x2*>(q) = f32x2{v[0], v[1]};
             else
 #pragma unroll
-                for (int k = 0; k < V; k += 4) *reinterpret_cast<f32x4*>(q + k) = f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]};
+                for (int k = 0; k < V; k += 4) put<PAST>(reinterpret_cast<f32x4*>(q + k), f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]});
         } else {
 #pragma unroll
             for (int k = 0; k < V; ++k)
@@ -187,84 +194,80 @@ __device__ __forceinline__ void finish(const LinearParams& p, int64_t m, int64_t
     store_values<VO>(p.out, p.out16, m * p.ldo + c, nc, o);
 }
 
-// A grouped call's tile: which expert, and its place among the expert's row tiles.
-struct Group {
-    int expert;
-    int first, end;  // the expert's rows
-    int tile;        // row tile within it
-};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
 
-// Row tiles of BM rows, the experts' one after the other; every lane of the wave calls it with the same
-// arguments.  Offsets outside [0, M] or decreasing are taken as an empty or a shorter group.
-struct GroupScan {
-    int cum, first, end;  // this lane's expert: tiles up to and with it, its rows
-    __device__ __forceinline__ void step(const LinearParams& p, int e0, int bm, int before) {
-        const int e = e0 + (threadIdx.x & 63), M = (int)p.g.M;
+// xcd_tile for fewer than 2^31 workgroups, which every launch here has: its divisions in 32 bits.
+__device__ __forceinline__ void xcd_tile32(uint32_t gx, uint32_t gy, int64_t& tn, int64_t& tm) {
+    const uint32_t T = gx * gy, i = blockIdx.x, k = i % 8, j = i / 8;
+    const uint32_t L = k * (T / 8) + min(k, T % 8) + j;
+    const uint32_t q = L / (4 * gx), r = L - q * 4 * gx, gm = min(gy - 4 * q, 4u);
+    const uint32_t n = gm == 4 ? r / 4 : r / gm;
+    tn = n;
+    tm = 4 * q + (r - n * gm);
+}
+
+// Experts e0 .. e0 + 63 of a grouped call, one a lane: its rows, and the row tiles of BM rows up to and with it, from
+// `before` on.  Offsets outside [0, M] or decreasing are taken as an empty or a shorter group.
+struct Groups {
+    int first, end, cum;
+    __device__ __forceinline__ Groups(const LinearParams& p, int e0, int bm, int before) {
+        const int lane = threadIdx.x & 63, e = e0 + lane, M = (int)p.g.M;
         first = end = 0;
         if (e < p.experts) {
-            first = min(max(p.offsets[e], 0), M);
-            end = min(max(p.offsets[e + 1], first), M);
+            const int a = p.offsets[e], b = p.offsets[e + 1];
+            first = min(max(a, 0), M);
+            end = min(max(b, first), M);
         }
-        int t = (end - first) / bm + ((end - first) % bm != 0);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(t, o);
-            if ((int)(threadIdx.x & 63) >= o) t += u;
-        }
-        cum = before + t;
+        cum = (end - first) / bm + ((end - first) % bm != 0);
+        cum = dpp_add<0x111, 0xf>(cum);  // row_shr 1, 2, 4, 8: sums up to the lane in its row of 16
+        cum = dpp_add<0x112, 0xf>(cum);
+        cum = dpp_add<0x114, 0xf>(cum);
+        cum = dpp_add<0x118, 0xf>(cum);
+        cum = dpp_add<0x142, 0xa>(cum);  // rows 0 and 2 onto 1 and 3, then 1 onto 2 and 3
+        cum = dpp_add<0x143, 0xc>(cum) + before;
     }
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(cum, 63); }
 };
-__device__ __forceinline__ int64_t group_tiles(const LinearParams& p, int bm) {
-    int total = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        GroupScan s;
-        s.step(p, e0, bm, total);
-        total = __builtin_amdgcn_readlane(s.cum, 63);
-    }
-    return total;
-}
-__device__ __forceinline__ Group find_group(const LinearParams& p, int bm, int tile) {
-    Group r{};
-    int before = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        GroupScan s;
-        s.step(p, e0, bm, before);
-        const uint64_t past = __ballot(s.cum > tile);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            r.expert = e0 + l;
-            r.first = __builtin_amdgcn_readlane(s.first, l);
-            r.end = __builtin_amdgcn_readlane(s.end, l);
-            r.tile = tile - (l ? __builtin_amdgcn_readlane(s.cum, l - 1) : before);
-            return r;
-        }
-        before = __builtin_amdgcn_readlane(s.cum, 63);
-    }
-    return r;
-}
 
 // The tile of workgroup blockIdx.x: its place in C, and p narrowed to its expert.  False: none is left
 // (the host's grid is the most that any offsets can need).
 template <bool GROUPED>
 __device__ __forceinline__ bool place(LinearParams& p, int bn, int bm, int64_t& nb0, int64_t& mb0) {
-    const int64_t gx = (p.g.N + bn - 1) / bn;
-    int64_t gy = (p.g.M + bm - 1) / bm, tn, tm;
-    if (GROUPED) {
-        gy = group_tiles(p, bm);
-        if (blockIdx.x >= gx * gy) return false;
+    const uint32_t gx = (uint32_t)((p.g.N + bn - 1) / bn);
+    int64_t tn, tm;
+    if (!GROUPED) {
+        xcd_tile32(gx, (uint32_t)((p.g.M + bm - 1) / bm), tn, tm);
+        nb0 = tn * bn;
+        mb0 = tm * bm;
+        return true;
     }
-    xcd_tile(gx, gy, tn, tm);
+    int e0 = 0, before = 0;
+    Groups g(p, 0, bm, 0);
+    int total = g.total();
+    const bool more = p.experts > 64;
+    for (int e = 64; e < p.experts; e += 64) total = Groups(p, e, bm, total).total();
+    if (blockIdx.x >= (uint64_t)gx * total) return false;
+    xcd_tile32(gx, (uint32_t)total, tn, tm);
+    while (more && g.total() <= tm) {  // (tm < total: it ends)
+        before = g.total();
+        e0 += 64;
+        g = Groups(p, e0, bm, before);
+    }
+    const uint64_t past = __ballot(g.cum > (int)tm);
+    if (!past) return false;
+    const int l = __builtin_ctzll(past), e = e0 + l;
+    const int first = __builtin_amdgcn_readlane(g.first, l), end = __builtin_amdgcn_readlane(g.end, l);
+    const int tile = (int)tm - (l ? __builtin_amdgcn_readlane(g.cum, l - 1) : before);
     nb0 = tn * bn;
-    mb0 = tm * bm;
-    if (GROUPED) {
-        const Group r = find_group(p, bm, (int)tm);
-        if (r.first >= r.end) return false;
-        mb0 = r.first + (int64_t)r.tile * bm;
-        p.g.M = r.end;
-        p.g.b_codes += r.expert * p.g.N * (p.g.K / 2);
-        p.g.b_scales += r.expert * p.g.N * (p.g.K / 32);
-        if (p.bias) p.bias = static_cast<const uint8_t*>(p.bias) + r.expert * p.g.N * (p.vec16 ? 2 : 4);
-    }
+    mb0 = first + (int64_t)tile * bm;
+    if (mb0 >= end) return false;
+    p.g.M = end;
+    p.g.b_codes += e * p.g.N * (p.g.K / 2);
+    p.g.b_scales += e * p.g.N * (p.g.K / 32);
+    if (p.bias) p.bias = static_cast<const uint8_t*>(p.bias) + e * p.g.N * (p.vec16 ? 2 : 4);
     return true;
 }
 
@@ -371,35 +374,39 @@ __device__ __forceinline__ void finish_tile(const LinearParams& p, uint8_t* lds,
                     }
                 return;
             }
+            auto rows = [&](auto past) KQ_INLINE {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                if (trow + k * STEP > last) break;
-                const int64_t m = mb0 + trow + k * STEP;
-                const float4 a = *reinterpret_cast<const float4*>(from + k * STEP * RS);
-                const float4 b = *reinterpret_cast<const float4*>(from + k * STEP * RS + 16);
-                const float v[V] = {a.x + bias[0], a.y + bias[1], a.z + bias[2], a.w + bias[3],
-                                    b.x + bias[4], b.y + bias[5], b.z + bias[6], b.w + bias[7]};
-                float o[VO];
+                for (int k = 0; k < CH; ++k) {
+                    if (trow + k * STEP > last) break;
+                    const int64_t m = mb0 + trow + k * STEP;
+                    const float4 a = *reinterpret_cast<const float4*>(from + k * STEP * RS);
+                    const float4 b = *reinterpret_cast<const float4*>(from + k * STEP * RS + 16);
+                    const float v[V] = {a.x + bias[0], a.y + bias[1], a.z + bias[2], a.w + bias[3],
+                                        b.x + bias[4], b.y + bias[5], b.z + bias[6], b.w + bias[7]};
+                    float o[VO];
 #pragma unroll
-                for (int e = 0; e < VO; ++e) o[e] = A == Act::Swiglu ? activate<A>(v[2 * e]) * v[2 * e + 1] : activate<A>(v[e]);
-                if (GROUPED) {
-                    if (p.row_scale) {
+                    for (int e = 0; e < VO; ++e) o[e] = A == Act::Swiglu ? activate<A>(v[2 * e]) * v[2 * e + 1] : activate<A>(v[e]);
+                    if (GROUPED) {
+                        if (p.row_scale) {
 #pragma unroll
-                        for (int e = 0; e < VO; ++e) o[e] *= scale[GROUPED ? k : 0];
+                            for (int e = 0; e < VO; ++e) o[e] *= scale[GROUPED ? k : 0];
+                        }
+                    } else {
+                        if (p.gate) {
+                            if (!one_gate) load_values<VO>(p.gate, p.vec16, m / p.gate_rows * p.gate_stride + c, VO, gate);
+#pragma unroll
+                            for (int e = 0; e < VO; ++e) o[e] *= gate[e];
+                        }
+                        if (p.residual) {
+#pragma unroll
+                            for (int e = 0; e < VO; ++e) o[e] += stored_value<VO>(res[GROUPED ? 0 : k], p.out16, e);
+                        }
                     }
-                } else {
-                    if (p.gate) {
-                        if (!one_gate) load_values<VO>(p.gate, p.vec16, m / p.gate_rows * p.gate_stride + c, VO, gate);
-#pragma unroll
-                        for (int e = 0; e < VO; ++e) o[e] *= gate[e];
-                    }
-                    if (p.residual) {
-#pragma unroll
-                        for (int e = 0; e < VO; ++e) o[e] += stored_value<VO>(res[GROUPED ? 0 : k], p.out16, e);
-                    }
+                    store_values<VO, decltype(past)::value>(p.out, p.out16, m * p.ldo + c, VO, o);
                 }
-                store_values<VO>(p.out, p.out16, m * p.ldo + c, VO, o);
-            }
+            };
+            if (p.stream_out) rows(std::true_type{});
+            else rows(std::false_type{});
         });
     };
     one_pass(std::integral_constant<int, 0>{});
@@ -467,20 +474,29 @@ __global__ __launch_bounds__(64 * WN * WK) void mxfp4_linear_rows_kernel(LinearP
     }
     struct Unit {
         uint4 w[2], x[2][TM];
-        uint32_t sw[2], sx[2][TM];
+        uint2 sw, sx[TM];  // the row's eight scales
+    };
+    auto scales = [&](const uint8_t* q, int64_t u) {
+        typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(1)));
+        if (8 * u + 8 <= nkb) {
+            const u32x2u v = *reinterpret_cast<const u32x2u*>(q + 8 * u);
+            return make_uint2(v.x, v.y);
+        }
+        // the last unit of a K that ends inside it: this lane's two blocks (the last one's for those past K)
+        const int64_t k = 8 * u + b;
+        return make_uint2((uint32_t)q[min(k, nkb - 1)] << (8 * b), (uint32_t)q[min(k + 4, nkb - 1)] << (8 * b));
     };
     auto load = [&](int64_t u, Unit& f) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int64_t k = min(8 * u + 4 * s + b, nkb - 1);  // blocks past K read the last one; masked below
             f.w[s] = *reinterpret_cast<const uint4*>(cw + 16 * k);
-            f.sw[s] = sw[k];
 #pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                f.x[s][j] = *reinterpret_cast<const uint4*>(cx[j] + 16 * k);
-                f.sx[s][j] = sx[j][k];
-            }
+            for (int j = 0; j < TM; ++j) f.x[s][j] = *reinterpret_cast<const uint4*>(cx[j] + 16 * k);
         }
+        f.sw = scales(sw, u);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) f.sx[j] = scales(sx[j], u);
     };
     f32x4m acc[TM];
 #pragma unroll
@@ -488,16 +504,18 @@ __global__ __launch_bounds__(64 * WN * WK) void mxfp4_linear_rows_kernel(LinearP
     auto multiply = [&](int64_t u, Unit& f) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (8 * u + 4 * s + b >= nkb) {  // zero codes, scale 1
+            uint32_t w = (s ? f.sw.y : f.sw.x) >> (8 * b);
+            const bool past = 8 * u + 4 * s + b >= nkb;  // zero codes, scale 1
+            if (past) {
                 f.w[s] = make_uint4(0u, 0u, 0u, 0u);
-                f.sw[s] = 127u;
-#pragma unroll
-                for (int j = 0; j < TM; ++j) f.sx[s][j] = 127u;
+                w = 127u;
             }
 #pragma unroll
-            for (int j = 0; j < TM; ++j)
+            for (int j = 0; j < TM; ++j) {
+                const uint32_t x = past ? 127u : (s ? f.sx[j].y : f.sx[j].x) >> (8 * b);
                 acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(Frag{f.w[s], 0u}), operand(Frag{f.x[s][j], 0u}),
-                                                                          acc[j], 4, 4, 0, (int)f.sw[s], 0, (int)f.sx[s][j]);
+                                                                          acc[j], 4, 4, 0, (int)w, 0, (int)x);
+            }
         }
     };
     Unit f[D];
@@ -546,18 +564,36 @@ static int64_t row_tiles(const LinearParams& p, int64_t bm) {
     return p.g.M / bm + std::min(p.experts, p.g.M);
 }
 
-enum class LinearTile { Rows16, Rows32, Rows64, Split32, Split64, Pipe128, Pipe256 };
+// K of a tile of a few rows is split over as many waves as it takes to have about this many, 22 on a CU.
+constexpr int64_t kRowsWaves = 22 * 256;
+// Tiles of bm rows that have work: a group of a few rows is one.
+static int64_t rows_tiles(const LinearParams& p, int64_t bm) {
+    return (p.g.N + 15) / 16 * (p.offsets ? std::min(p.experts, p.g.M) : (p.g.M + bm - 1) / bm);
+}
+
+// Tile of a call.  Measured, us (bf16 out, weights not in the caches).
+// A few rows, K x N 3072 x 12288 / 12288 x 3072 / 1152 x 4608, tiles of 16 (32) rows and tiles that split K: 1 row 9.0,
+// 10.1, 4.4 and 10.1 (64 x 64), 15.9, 4.3 (32 x 32); 16 rows 10.6, 12.9, - and 13.6, -, -; 32 rows 15.3, 17.4, 5.2
+// and 13.5, 26.8, 4.6; 64 rows 22.5, 26.2, 6.8 (tiles of 64) and 16.3, 24.6, 6.4.  Waves that split K, 1 row: 8, 4, 2,
+// 1: 9.4, 9.0, 9.6, 15.4; 10.1, 15.3, 25.2, 47.7; 4.4, 4.4, 5.1, 6.5.
+// Grouped, tiles of 16 rows and 128 x 128: 64 experts of 2048 x 2816, 1, 2, 4, 8 rows an expert 31.3, 38.4, 49.2, 58.2
+// and 32.0, 38.4, 44.3, 51.6 (tiles that split K: 41.7 at 1 row); 8 experts of 2240 x 5600, 1, 2, 4, 8, 16 rows
+// 13.1, 17.5, 19.6, 23.5, 29.4 and 16.5, 20.9, 22.4, 23.6, 25.1.
+// More rows: as mxfp4_gemm's tiles; 128 x 128 and 256 x 256, grouped 32 experts 12004 x 1152 x 2240 fp32 71, 71,
+// 16 experts 16384 x 2240 x 5600 258, 216.
+enum class LinearTile { Rows16, Rows32, Split32, Split64, Pipe128, Pipe256 };
 
 static LinearTile linear_tile_of(const LinearParams& p) {
     const GemmParams& g = p.g;
     auto tiles = [&](int64_t tm, int64_t tn) { return row_tiles(p, tm) * ((g.N + tn - 1) / tn); };
-    // rows that share a weight: those of the average group
-    const int64_t rows = p.offsets ? (g.M + p.experts - 1) / p.experts : g.M;
-    if (rows <= 16) return LinearTile::Rows16;
-    if (rows <= 32) return LinearTile::Rows32;
-    if (rows <= 64) return LinearTile::Rows64;
     // gathered pipelined tiles have 32-bit offsets into all of A
     const bool pipe = g.K <= kPipeMaxK && (!g.rows || g.a_rows <= (int64_t(1) << 32) / (g.K / 2));
+    if (p.offsets) {
+        if (g.M <= p.experts * (rows_tiles(p, 16) <= kRowsWaves ? 8 : 2)) return LinearTile::Rows16;
+    } else {
+        if (g.M <= 16) return LinearTile::Rows16;
+        if (g.M <= 32 && g.K > 4096) return LinearTile::Rows32;
+    }
     if (tiles(32, 32) <= 256) return LinearTile::Split32;
     if (tiles(64, 64) <= 256 || !pipe) return LinearTile::Split64;
     const int64_t rounds128 = (tiles(128, 128) + 511) / 512, rounds256 = (tiles(256, 256) + 255) / 256;
@@ -580,6 +616,15 @@ static void launch_rows(const LinearParams& p, hipStream_t st) {
         hipLaunchKernelGGL((mxfp4_linear_rows_kernel<TM, WN, WK, D, decltype(grouped)::value, decltype(gather)::value>), grid,
                            dim3(64 * WN * WK), 0, st, p);
     });
+}
+
+template <int TM, int D>
+static void launch_rows_by_waves(const LinearParams& p, hipStream_t st) {
+    const int64_t split = std::min(kRowsWaves / rows_tiles(p, 16 * TM), (p.g.K + 255) / 256);
+    if (split >= 8) launch_rows<TM, 1, 8, D>(p, st);
+    else if (split >= 4) launch_rows<TM, 2, 4, D>(p, st);
+    else if (split >= 2) launch_rows<TM, 4, 2, D>(p, st);
+    else launch_rows<TM, 8, 1, D>(p, st);
 }
 
 template <int TN, int TM, int W, int D>
@@ -606,11 +651,21 @@ static void launch_pipe(const LinearParams& p, hipStream_t st) {
 
 int64_t mxfp4_grouped_workgroups(const LinearParams& p) { return (p.g.N + 15) / 16 * row_tiles(p, 16); }
 
-hipError_t launch_mxfp4_linear(const LinearParams& p, hipStream_t st) {
+// Bytes that a call reads and writes.
+static int64_t touched(const LinearParams& p) {
+    const int64_t cols = p.act == Act::Swiglu ? p.g.N / 2 : p.g.N, out = p.g.M * cols * (p.out16 ? 2 : 4);
+    const int64_t weights = p.offsets ? std::min(p.experts, p.g.M) : 1;
+    return (std::min(p.g.rows ? p.g.a_rows : p.g.M, p.g.M) + weights * p.g.N) * (p.g.K / 2) + (p.residual ? 2 : 1) * out;
+}
+
+hipError_t launch_mxfp4_linear(LinearParams p, hipStream_t st) {
+    // Half of the 256 MB memory-side cache: past it an output that is kept there drives out what the next tiles
+    // read.  us, kept and not: grouped 12004 x 1152 x 2240 fp32 with 32 experts (159 MB) 72, 52; 4608 x 3072 x 12288
+    // (141 MB) 140, 132; 12004 x 1152 x 2240 fp32, one weight (115 MB), onto the same output each time 46, 54.
+    p.stream_out = touched(p) > (int64_t(128) << 20);
     switch (linear_tile_of(p)) {
-        case LinearTile::Rows16: launch_rows<1, 1, 8, 3>(p, st); break;
-        case LinearTile::Rows32: launch_rows<2, 1, 8, 3>(p, st); break;
-        case LinearTile::Rows64: launch_rows<4, 1, 8, 2>(p, st); break;
+        case LinearTile::Rows16: launch_rows_by_waves<1, 3>(p, st); break;
+        case LinearTile::Rows32: launch_rows_by_waves<2, 3>(p, st); break;
         case LinearTile::Split32: launch_split<1, 1, 8, 4>(p, st); break;
         case LinearTile::Split64: launch_split<2, 2, 8, 2>(p, st); break;
         case LinearTile::Pipe128: launch_pipe<2, 2, 2, 2, false>(p, st); break;

@@ -23,6 +23,7 @@ def _linear(**kw):
     (dict(M=1 << 31), INVALID), (dict(N=65535 * 128 + 1, ldo=1 << 40), INVALID), (dict(vt=2), INVALID), (dict(ot=-1), INVALID),
     (dict(act=6), INVALID), (dict(act=-1), INVALID), (dict(act=5, N=5), INVALID), (dict(ldo=5), INVALID), (dict(act=5, ldo=2), INVALID),
     (dict(gate=FAKE, gr=0), INVALID), (dict(gate=FAKE, gs=-1), INVALID), (dict(res=FAKE, ldr=5), INVALID),
+    (dict(M=(1 << 31) - 1, N=1 << 20, ldo=1 << 20), UNSUPPORTED),  # 2^25 x 2^14 tiles of 64 x 64
     (dict(ac=None), NULLP), (dict(as_=None), NULLP), (dict(bc=None), NULLP), (dict(bs=None), NULLP), (dict(out=None), NULLP),
     (dict(ac=FAKE + 8), MISALIGNED), (dict(bc=FAKE + 1), MISALIGNED), (dict(out=FAKE + 1), MISALIGNED),
     (dict(bias=FAKE + 2), MISALIGNED), (dict(gate=FAKE + 2), MISALIGNED), (dict(res=FAKE + 1, ldr=6), MISALIGNED),
