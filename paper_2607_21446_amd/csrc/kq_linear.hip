@@ -448,7 +448,8 @@ __global__ __launch_bounds__(64 * W) void mxfp4_linear_split_kernel(LinearParams
     });
 }
 
-// A few rows (a decoding step): the weight is read once and bounds the call.  A tile is 16 TM rows of A
+// A few rows (a decoding step): the weight is read once and bounds the call (64 experts of 2048 x 2816 for 64 rows,
+// 196 MB: 29 us, 6.8 TB/s; one row through 3072 x 12288, 20 MB: 7.9 us, of which an empty launch is 3).  A tile is 16 TM rows of A
 // by 16 of B; v_mfma_scale_f32_16x16x128_f8f6f4 takes lane l's 16 code bytes as row l % 16, block l / 16
 // of the 128-wide K step, so fragments are plain loads.  WN waves have a tile each, next to each other
 // along N, and WK waves split each tile's K, in units of 256 (whole 128-byte lines of B), D units in flight;
@@ -572,15 +573,17 @@ static int64_t rows_tiles(const LinearParams& p, int64_t bm) {
 }
 
 // Tile of a call.  Measured, us (bf16 out, weights not in the caches).
-// A few rows, K x N 3072 x 12288 / 12288 x 3072 / 1152 x 4608, tiles of 16 (32) rows and tiles that split K: 1 row 9.0,
-// 10.1, 4.4 and 10.1 (64 x 64), 15.9, 4.3 (32 x 32); 16 rows 10.6, 12.9, - and 13.6, -, -; 32 rows 15.3, 17.4, 5.2
-// and 13.5, 26.8, 4.6; 64 rows 22.5, 26.2, 6.8 (tiles of 64) and 16.3, 24.6, 6.4.  Waves that split K, 1 row: 8, 4, 2,
-// 1: 9.4, 9.0, 9.6, 15.4; 10.1, 15.3, 25.2, 47.7; 4.4, 4.4, 5.1, 6.5.
-// Grouped, tiles of 16 rows and 128 x 128: 64 experts of 2048 x 2816, 1, 2, 4, 8 rows an expert 31.3, 38.4, 49.2, 58.2
+// A few rows, K x N 3072 x 12288 / 12288 x 3072 / 1152 x 4608: tiles of 16 (32) rows and the best that splits K: 1 row
+// 7.9, 10.1, 4.4 and 10.1 (64 x 64), 15.9, 4.3 (32 x 32); 16 rows 9.6, 12.9, - and 13.6, -, -; 32 rows 15.3, 17.4, 5.2
+// and 13.5, 26.8, 4.6; 64 rows 22.5, 26.2, 6.8 (tiles of 64 rows, not kept) and 16.3, 24.6, 6.4.
+// Waves that split K, 8, 4, 2, 1: 1 row 9.2, 7.9, 9.6, 14.0; 10.1, 12.4, -, -; 8 of 64 experts of 2048 x 2816, a row each
+// 14.7, 10.7, 9.8, 12.0; all 64 56, 35.2, 29.5, 29.0; 8 experts of 2240 x 5600, 2 rows each -, 15.7, 15.5, 17.4.
+// Workgroups of 8 waves where these have 4: 1 row 9.0; 64 experts 30.6; 8 experts 16.9 us.
+// Grouped, tiles of 16 rows and 128 x 128: 64 experts of 2048 x 2816, 1, 2, 4, 8 rows an expert 29.0, 38.4, 49.2, 58.2
 // and 32.0, 38.4, 44.3, 51.6 (tiles that split K: 41.7 at 1 row); 8 experts of 2240 x 5600, 1, 2, 4, 8, 16 rows
-// 13.1, 17.5, 19.6, 23.5, 29.4 and 16.5, 20.9, 22.4, 23.6, 25.1.
-// More rows: as mxfp4_gemm's tiles; 128 x 128 and 256 x 256, grouped 32 experts 12004 x 1152 x 2240 fp32 71, 71,
-// 16 experts 16384 x 2240 x 5600 258, 216.
+// 13.1, 15.5, 19.6, 23.5, 29.4 and 16.5, 20.9, 22.4, 23.6, 25.1.
+// More rows: as mxfp4_gemm's tiles; 128 x 128 and 256 x 256, grouped 32 experts 12004 x 1152 x 2240 fp32 52, 65,
+// 16 experts 16384 x 2240 x 5600 256, 219.
 enum class LinearTile { Rows16, Rows32, Split32, Split64, Pipe128, Pipe256 };
 
 static LinearTile linear_tile_of(const LinearParams& p) {
@@ -622,9 +625,9 @@ template <int TM, int D>
 static void launch_rows_by_waves(const LinearParams& p, hipStream_t st) {
     const int64_t split = std::min(kRowsWaves / rows_tiles(p, 16 * TM), (p.g.K + 255) / 256);
     if (split >= 8) launch_rows<TM, 1, 8, D>(p, st);
-    else if (split >= 4) launch_rows<TM, 2, 4, D>(p, st);
-    else if (split >= 2) launch_rows<TM, 4, 2, D>(p, st);
-    else launch_rows<TM, 8, 1, D>(p, st);
+    else if (split >= 4) launch_rows<TM, 1, 4, D>(p, st);
+    else if (split >= 2) launch_rows<TM, 2, 2, D>(p, st);
+    else launch_rows<TM, 4, 1, D>(p, st);
 }
 
 template <int TN, int TM, int W, int D>
