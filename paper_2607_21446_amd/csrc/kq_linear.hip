@@ -26,7 +26,7 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 // act(p).  The exponentials and reciprocals are the hardware's (1 ulp each).
 template <Act A>
 __device__ __forceinline__ float activate(float p) {
-    if (A == Act::Relu) return fmaxf(p, 0.0f);
+    if (A == Act::Relu) return p <= 0.0f ? 0.0f : p;  // NaN stays NaN, as in the other activations
     if (A == Act::Silu || A == Act::Swiglu) return p * sigmoid(p);
     if (A == Act::GeluTanh) {
         // p (1 + tanh z) / 2 = p sigmoid(2 z), z = sqrt(2 / pi) (p + 0.044715 p^3)
@@ -251,7 +251,8 @@ __device__ __forceinline__ bool place(LinearParams& p, int bn, int bm, int64_t& 
     for (int e = 64; e < p.experts; e += 64) total = Groups(p, e, bm, total).total();
     if (blockIdx.x >= (uint64_t)gx * total) return false;
     xcd_tile32(gx, (uint32_t)total, tn, tm);
-    while (more && g.total() <= tm) {  // (tm < total: it ends)
+    // (with offsets as they should be, tm < total ends it; sums of others may pass 32 bits)
+    while (more && g.total() <= tm && e0 + 64 < p.experts) {
         before = g.total();
         e0 += 64;
         g = Groups(p, e0, bm, before);

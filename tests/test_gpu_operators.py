@@ -620,3 +620,28 @@ def test_linear_past_32_bit_offsets():
         w = _values(b[0][e, N - 100:], b[1][e, N - 100:])
         want, err = _product_and_error(av[rows[r:r + 1].long()], w, None, None)
         _within(out[r:r + 1, N - 100:], want, err, "expert")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M,N", [(1, 20), (200, 260), (2304, 2304)])
+def test_linear_keeps_nan(act, M, N):
+    """A NaN in the bias comes out in its column, and in no other."""
+    g = _gen(18)
+    bias = _randn(g, N)
+    bias[2] = float("nan")
+    out = kq.mxfp4_linear(*_codes(g, M, 256), *_codes(g, N, 256), bias=bias, act=act)
+    assert torch.isnan(out[:, 1 if act == "swiglu" else 2]).all() and int(torch.isnan(out).sum()) == M
+
+
+def test_grouped_bad_offsets_of_many_experts():
+    """Offsets that go up and down over more than 64 experts ask for more tiles than a call launches: it ends, and
+    writes nothing outside the output."""
+    g = _gen(19)
+    E, R, N, K = 200, 3000, 64, 64
+    a, b = _codes(g, R, K), _codes(g, E, N, K)
+    off = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    off[1::2] = R
+    out = torch.full((R + 1, N), 7.0, dtype=BF16, device="cuda")
+    kq.mxfp4_grouped_linear(*a, *b, off, out=out[:R])
+    torch.cuda.synchronize()
+    assert (out[R] == 7.0).all() and torch.isfinite(out[:R]).all()
