@@ -350,9 +350,11 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(const NormParams p)
             const float q = centre(v, at, p.post == 2, slots[2 * turn], rest);
             const float r = inverse_root(q, at.inv_d, p.eps);
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[j][k] = (v[j][k] + rest) * r;
+                if (p.post == 2) at.clip(j, v[j]);  // rest reaches past the row's end too, where the second norm sums zeros
+            }
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
