@@ -479,7 +479,8 @@ PyObject* mxfp4_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
         Vectors vec(o.dev);
         const void *bias, *gate;
         int64_t none, stride;
-        if (!vec.add(v[4], o.N, false, &bias, &none) || !vec.add(v[6], cols, true, &gate, &stride) || o.M % vec.count()) return nullptr;
+        if (!vec.add(v[4], o.N, false, &bias, &none) || !vec.add(v[6], cols, true, &gate, &stride)) return nullptr;
+        if (vec.count() <= 0 || o.M % vec.count()) return nullptr;
         at::ScalarType type = at::kBFloat16;
         const at::Tensor* res = nullptr;
         if (v[7] != Py_None) {
