@@ -520,8 +520,8 @@ def block_norm(x, residual=None, gate=None, post_weight=None, weight=None, scale
     another of the two if need be (h of residual's type, else ``h_dtype``, else x's).
     gate, scale and shift [d] or [B, d] for B equal batches of rows (slices of one
     modulation tensor), weight and post_weight [d], all of one type.  h may be
-    residual and y may be x.  Where h would be x itself it is not written, and x
-    is returned for it.  Returns (h, y)."""
+    residual and y may be x.  Where h would be x itself, and y is not, it is not
+    written, and x is returned for it.  Returns (h, y)."""
     kind, post = _one_of(_NORMS, norm, "norm"), _one_of(_NORMS, post_norm, "post_norm")
     r = _native().block_norm(x, residual, gate, post_weight, weight, scale, shift, kind, post, alpha, eps, h, y, h_dtype,
                              stream)
@@ -536,7 +536,8 @@ def block_norm(x, residual=None, gate=None, post_weight=None, weight=None, scale
     if residual is not None:
         _same(residual, x, "residual", residual.dtype)
         h_dtype = residual.dtype
-    plain = residual is None and gate is None and not post and alpha == 1.0 and h is None and h_dtype in (None, x.dtype)
+    plain = (residual is None and gate is None and not post and alpha == 1.0 and h is None and h_dtype in (None, x.dtype)
+             and (y is None or y.data_ptr() != x.data_ptr()))
     if h is None and not plain:
         h = torch.empty((M, d), dtype=h_dtype or x.dtype, device=x.device)
     if h is not None:

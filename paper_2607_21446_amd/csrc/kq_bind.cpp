@@ -592,7 +592,9 @@ PyObject* block_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
         }
         NormVectors vs(x->device());
         if (!vs.parse(v + 2, M, d)) return nullptr;
-        const bool plain = !res && !vs.gate && !post && alpha == 1.0f && ht == xt && v[11] == Py_None;
+        const at::Tensor* const over = tensor(v[12]);  // h is x itself, unless y goes over it
+        const bool plain = !res && !vs.gate && !post && alpha == 1.0f && ht == xt && v[11] == Py_None &&
+                           !(over && over->data_ptr() == x->data_ptr());
         Out h, y;
         const at::ScalarType hs = ht == KQ_DTYPE_BF16 ? at::kBFloat16 : at::kFloat;
         if (v[11] != Py_None) {

@@ -22,6 +22,13 @@ def _codes(*shape):
             torch.full((*lead, K // 32), 127, dtype=torch.uint8, device="cuda"))
 
 
+class _NoNative:
+    """Stands for the binding's native part and takes no call."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 @pytest.mark.parametrize("M", [0, 4])
 def test_vectors_of_no_batches_are_refused(M):
     """A gate [0, N] belongs to no row: an error that names it, and no division by the number of batches."""
@@ -39,3 +46,25 @@ def test_vectors_of_no_batches_are_refused(M):
             kq.block_norm(x, x, **{name: none})
         with pytest.raises(ValueError, match="0 batches"):
             kq.block_norm_backward(x, x, x=x, **{name: none})
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("M,d", [(5, 64), (3, 1155), (300, 1152)])
+def test_the_stream_outlives_a_norm_in_place(monkeypatch, native, norm, M, d):
+    """y over x, with nothing that makes h another array than x: h still holds what x held."""
+    from paper_2607_21446_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_native", _NoNative)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M + d)
+    x = torch.randn((M, d), generator=g, device="cuda").to(torch.bfloat16)
+    was = x.clone()
+    _, want = kq.block_norm(x, norm=norm)
+    assert torch.equal(x, was)
+    h, y = kq.block_norm(x, norm=norm, y=x)
+    assert y is x and torch.equal(y, want)
+    assert h is not x and torch.equal(h, was)
+    view = was.clone()
+    h, y = kq.block_norm(view, norm=norm, y=view[:])  # the same memory by another tensor
+    assert torch.equal(h, was) and torch.equal(view, want)
