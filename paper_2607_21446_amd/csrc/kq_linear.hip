@@ -9,6 +9,7 @@
 
 #include "kq_gemm_tile.h"
 #include "kq_linear.h"
+#include "kq_place.h"
 
 namespace kq {
 
@@ -192,84 +193,6 @@ __device__ __forceinline__ void finish(const LinearParams& p, int64_t m, int64_t
         }
     }
     store_values<VO>(p.out, p.out16, m * p.ldo + c, nc, o);
-}
-
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add(int v) {
-    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
-}
-
-// xcd_tile for fewer than 2^31 workgroups, which every launch here has: its divisions in 32 bits.
-__device__ __forceinline__ void xcd_tile32(uint32_t gx, uint32_t gy, int64_t& tn, int64_t& tm) {
-    const uint32_t T = gx * gy, i = blockIdx.x, k = i % 8, j = i / 8;
-    const uint32_t L = k * (T / 8) + min(k, T % 8) + j;
-    const uint32_t q = L / (4 * gx), r = L - q * 4 * gx, gm = min(gy - 4 * q, 4u);
-    const uint32_t n = gm == 4 ? r / 4 : r / gm;
-    tn = n;
-    tm = 4 * q + (r - n * gm);
-}
-
-// Experts e0 .. e0 + 63 of a grouped call, one a lane: its rows, and the row tiles of BM rows up to and with it, from
-// `before` on.  Offsets outside [0, M] or decreasing are taken as an empty or a shorter group.
-struct Groups {
-    int first, end, cum;
-    __device__ __forceinline__ Groups(const LinearParams& p, int e0, int bm, int before) {
-        const int lane = threadIdx.x & 63, e = e0 + lane, M = (int)p.g.M;
-        first = end = 0;
-        if (e < p.experts) {
-            const int a = p.offsets[e], b = p.offsets[e + 1];
-            first = min(max(a, 0), M);
-            end = min(max(b, first), M);
-        }
-        cum = (end - first) / bm + ((end - first) % bm != 0);
-        cum = dpp_add<0x111, 0xf>(cum);  // row_shr 1, 2, 4, 8: sums up to the lane in its row of 16
-        cum = dpp_add<0x112, 0xf>(cum);
-        cum = dpp_add<0x114, 0xf>(cum);
-        cum = dpp_add<0x118, 0xf>(cum);
-        cum = dpp_add<0x142, 0xa>(cum);  // rows 0 and 2 onto 1 and 3, then 1 onto 2 and 3
-        cum = dpp_add<0x143, 0xc>(cum) + before;
-    }
-    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(cum, 63); }
-};
-
-// The tile of workgroup blockIdx.x: its place in C, and p narrowed to its expert.  False: none is left
-// (the host's grid is the most that any offsets can need).
-template <bool GROUPED>
-__device__ __forceinline__ bool place(LinearParams& p, int bn, int bm, int64_t& nb0, int64_t& mb0) {
-    const uint32_t gx = (uint32_t)((p.g.N + bn - 1) / bn);
-    int64_t tn, tm;
-    if (!GROUPED) {
-        xcd_tile32(gx, (uint32_t)((p.g.M + bm - 1) / bm), tn, tm);
-        nb0 = tn * bn;
-        mb0 = tm * bm;
-        return true;
-    }
-    int e0 = 0, before = 0;
-    Groups g(p, 0, bm, 0);
-    int total = g.total();
-    const bool more = p.experts > 64;
-    for (int e = 64; e < p.experts; e += 64) total = Groups(p, e, bm, total).total();
-    if (blockIdx.x >= (uint64_t)gx * total) return false;
-    xcd_tile32(gx, (uint32_t)total, tn, tm);
-    // (with offsets as they should be, tm < total ends it; sums of others may pass 32 bits)
-    while (more && g.total() <= tm && e0 + 64 < p.experts) {
-        before = g.total();
-        e0 += 64;
-        g = Groups(p, e0, bm, before);
-    }
-    const uint64_t past = __ballot(g.cum > (int)tm);
-    if (!past) return false;
-    const int l = __builtin_ctzll(past), e = e0 + l;
-    const int first = __builtin_amdgcn_readlane(g.first, l), end = __builtin_amdgcn_readlane(g.end, l);
-    const int tile = (int)tm - (l ? __builtin_amdgcn_readlane(g.cum, l - 1) : before);
-    nb0 = tn * bn;
-    mb0 = first + (int64_t)tile * bm;
-    if (mb0 >= end) return false;
-    p.g.M = end;
-    p.g.b_codes += e * p.g.N * (p.g.K / 2);
-    p.g.b_scales += e * p.g.N * (p.g.K / 32);
-    if (p.bias) p.bias = static_cast<const uint8_t*>(p.bias) + e * p.g.N * (p.vec16 ? 2 : 4);
-    return true;
 }
 
 }  // namespace
@@ -560,10 +483,9 @@ __global__ __launch_bounds__(64 * WN * WK) void mxfp4_linear_rows_kernel(LinearP
 
 constexpr int64_t kPipeMaxK = int64_t(1) << 24;  // 32-bit offsets within a tile
 
-// Row tiles that a call can need: every group may end inside one.
+// Row tiles that a call can need.
 static int64_t row_tiles(const LinearParams& p, int64_t bm) {
-    if (!p.offsets) return (p.g.M + bm - 1) / bm;
-    return p.g.M / bm + std::min(p.experts, p.g.M);
+    return p.offsets ? group_tiles(p.g.M, p.experts, bm) : (p.g.M + bm - 1) / bm;
 }
 
 // K of a tile of a few rows is split over as many waves as it takes to have about this many, 22 on a CU.
