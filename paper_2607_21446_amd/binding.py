@@ -12,6 +12,7 @@ workspace is marshalled here.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from functools import lru_cache
@@ -126,6 +127,16 @@ def _stream(stream):
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _scratch_of(stream, device):
+    """In here torch allocates in the order of the call's stream: what a call drops while its kernels may still run
+    (a workspace of its own) is given again to that stream only, and so after them."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 def _need(t, dtype, name, device=True):
@@ -596,7 +607,8 @@ def block_norm_backward(dy, h, dh=None, x=None, gate=None, post_weight=None, wei
     if dx is not None:
         _same(dx, dy, "dx")
     if workspace is None:
-        workspace = block_norm_workspace(M, d, B, dy.device)
+        with _scratch_of(stream, dy.device):
+            workspace = block_norm_workspace(M, d, B, dy.device)
     _need(workspace, torch.uint8, "workspace")
     if workspace.device != dy.device:
         raise ValueError(f"workspace is on {workspace.device}, the input on {dy.device}")
@@ -787,7 +799,8 @@ def calib_step(X, W, Yneg, lu, lambdas, a=4, workspace=None, adam=None, grad=Non
     R, d, o, nfac = _calib_shapes(X, W, Yneg, lu)
     _size(lambdas, 2, "lambdas", X.device)
     if workspace is None:
-        workspace = calib_workspace(R, o, d, a, nfac, X.device)
+        with _scratch_of(stream, X.device):
+            workspace = calib_workspace(R, o, d, a, nfac, X.device)
     _need(workspace, torch.uint8, "workspace")
     if grad is None:
         grad = torch.empty((nfac, 5, 3), dtype=torch.float32, device=X.device)
@@ -858,10 +871,12 @@ def calibrate(X, W, lu=None, a=4, per_block=True, steps=100, lr=1e-2, Yneg=None,
         lu = hadamard_lu(d // 32 if per_block else 1, X.device)
     _need(lu, torch.float32, "lu")
     if Yneg is None:
-        Yneg = calib_reference(X, W, stream=stream)
+        with _scratch_of(stream, X.device):
+            Yneg = calib_reference(X, W, stream=stream)
     R, d, o, nfac = _calib_shapes(X, W, Yneg, lu)
     if workspace is None:
-        workspace = calib_workspace(R, o, d, a, nfac, X.device)
+        with _scratch_of(stream, X.device):
+            workspace = calib_workspace(R, o, d, a, nfac, X.device)
     _need(workspace, torch.uint8, "workspace")
     losses = torch.empty((steps + 2, 4), dtype=torch.float64, device=X.device)
     _check(lib().kq_calibrate(_ptr(X), R, d, _ptr(W), o, _ptr(Yneg), _ptr(lu), a, nfac, int(steps), float(lr),

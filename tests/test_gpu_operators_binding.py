@@ -68,3 +68,51 @@ def test_the_stream_outlives_a_norm_in_place(monkeypatch, native, norm, M, d):
     view = was.clone()
     h, y = kq.block_norm(view, norm=norm, y=view[:])  # the same memory by another tensor
     assert torch.equal(h, was) and torch.equal(view, want)
+
+
+@pytest.mark.parametrize("kind", ["object", "handle", "default", "current"])
+def test_a_workspace_of_the_call_is_its_streams(monkeypatch, kind):
+    """Without a workspace a call makes one and drops it while its kernels may still run: its memory belongs to the
+    stream that they run on, so that no work of another stream is given it."""
+    from paper_2607_21446_amd import binding
+    side = torch.cuda.Stream()
+    stream = {"object": side, "handle": side.cuda_stream, "default": 0, "current": None}[kind]
+    at = {"object": side, "handle": side}.get(kind, torch.cuda.default_stream()).cuda_stream
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    bf16 = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    x, h, dy, w = bf16(96, 512), bf16(96, 512), bf16(96, 512), bf16(512)
+    X, W = bf16(64, 128), bf16(96, 128)
+    lam = torch.tensor([0.5, 0.25], device="cuda")
+    lu = kq.hadamard_lu(1)
+    Y, mine = kq.calib_reference(X, W), lu.clone()
+    calls = [lambda **k: list(kq.block_norm_backward(dy, h, x=x, gate=w, weight=w, **k).values()),
+             lambda **k: list(kq.calib_step(X, W, Y, lu, lam, a=4, **k)),
+             lambda **k: list(kq.calibrate(X, W, lu=mine, a=4, steps=2, **k))]
+    want = [[t.clone() for t in c()] for c in calls]
+    made = []
+
+    def noted(name):
+        real = getattr(binding, name)
+
+        def f(*args):
+            t = real(*args)
+            made.append((torch.cuda.current_stream().cuda_stream, t.data_ptr(), t.numel()))
+            return t
+        monkeypatch.setattr(binding, name, f)
+
+    noted("block_norm_workspace")
+    noted("calib_workspace")
+    for i, c in enumerate(calls):
+        made.clear()
+        mine.copy_(lu)
+        torch.cuda.synchronize()  # the other stream takes no inputs that are still being written
+        got = c(stream=stream)
+        assert len(made) == 1 and made[0][0] == at, i
+        assert torch.cuda.current_stream() == torch.cuda.default_stream()
+        if at == side.cuda_stream:  # dropped, and not given to the current stream
+            t = torch.empty(made[0][2], dtype=torch.uint8, device="cuda")
+            assert t.data_ptr() != made[0][1], i
+        torch.cuda.synchronize()
+        for a, b in zip(got, want[i], strict=True):
+            assert torch.equal(a, b), i
