@@ -116,3 +116,117 @@ def test_a_workspace_of_the_call_is_its_streams(monkeypatch, kind):
         torch.cuda.synchronize()
         for a, b in zip(got, want[i], strict=True):
             assert torch.equal(a, b), i
+
+
+class _Recorder:
+    """The native part; every call that it makes is noted, None for one that it leaves to Python."""
+
+    def __init__(self, native):
+        self.native, self.taken = native, []
+
+    def __getattr__(self, name):
+        def f(*args):
+            r = getattr(self.native, name)(*args)
+            self.taken.append(None if r is None else name)
+            return r
+        return f
+
+
+def _calls():
+    """Name, call with buffers of its own (given) or none, and which results are then the caller's."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    bf16 = lambda *s: randn(*s).to(torch.bfloat16)  # noqa: E731
+    M, d = 12, 150
+    x, res, mod, w = bf16(M, d), randn(M, d), bf16(3, 6 * d), bf16(d)
+    norm_args = dict(gate=mod[:, :d], scale=mod[:, d:2 * d], shift=mod[:, 2 * d:3 * d], weight=w)
+    new = lambda dtype, *s: torch.full(s, 7.0, dtype=dtype, device="cuda")  # noqa: E731
+
+    def norm(given, stream, **kw):
+        k = dict(h=new(torch.float32, M, d), y=new(torch.bfloat16, M, d)) if given else {}
+        out = kq.block_norm(x, res, **kw, **k, stream=stream)
+        return out, [k["h"], k["y"]] if given else None
+
+    def plain_norm(given, stream):
+        return kq.block_norm(x, weight=w, norm="rms", stream=stream, **(dict(y=new(torch.bfloat16, M, d)) if given else {})), None
+
+    K, N, E = 96, 70, 3
+    random = lambda *s: torch.randint(0, 256, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    scales = lambda *s: torch.randint(123, 128, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    a, b, be = (random(M, K // 2), scales(M, K // 32)), (random(N, K // 2), scales(N, K // 32)), (random(E, N, K // 2), scales(E, N, K // 32))
+    off = torch.tensor([0, 5, 5, 20], dtype=torch.int32, device="cuda")
+    rows = torch.randint(0, M, (20,), generator=g, device="cuda").to(torch.int32)
+    bias, biases, row_scale, gate = randn(N), bf16(E, N), randn(20), randn(2, N + 9)[:, 4:4 + N]
+
+    def linear(given, stream, act, **kw):
+        n = N // 2 if act == "swiglu" else N
+        residual = new(torch.float32, M, n + 3)[:, 1:n + 1] if "gate" in kw else None
+        out = new(torch.float32, M, n + 5)[:, 2:n + 2] if given else None
+        r = kq.mxfp4_linear(*a, *b, bias=bias, act=act, residual=residual, out=out, out_dtype=torch.float32, stream=stream, **kw)
+        return (r,), [out] if given else None
+
+    def grouped(given, stream, act, **kw):
+        n = N // 2 if act == "swiglu" else N
+        out = new(torch.bfloat16, 20 if "rows" in kw else M, n) if given else None
+        o = off if "rows" in kw else off.clamp_max(M)
+        r = kq.mxfp4_grouped_linear(*a, *be, o, act=act, out=out, stream=stream, **kw)
+        return (r,), [out] if given else None
+
+    return [("block_norm", lambda g_, s: norm(g_, s, norm="layer", post_norm="layer", post_weight=w, alpha=0.5, **norm_args)),
+            ("block_norm", lambda g_, s: norm(g_, s, norm="rms")),
+            ("block_norm", plain_norm),
+            ("mxfp4_linear", lambda g_, s: linear(g_, s, "gelu")),
+            ("mxfp4_linear", lambda g_, s: linear(g_, s, None, gate=gate)),
+            ("mxfp4_linear", lambda g_, s: linear(g_, s, "swiglu")),
+            ("mxfp4_grouped_linear", lambda g_, s: grouped(g_, s, "swiglu", rows=rows, row_scale=row_scale)),
+            ("mxfp4_grouped_linear", lambda g_, s: grouped(g_, s, None, bias=biases))]
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_native_marshalling_matches_python(monkeypatch, given):
+    """The native part takes these calls, and the checks and the ctypes call in Python return the same: values, types
+    and, for buffers that were given, the same objects."""
+    from paper_2607_21446_amd import binding
+    stream = torch.cuda.current_stream().cuda_stream if given else None
+    recorder = _Recorder(binding._native())
+    for i, (name, call) in enumerate(_calls()):
+        recorder.taken.clear()
+        monkeypatch.setattr(binding, "_native", lambda: recorder)
+        got, mine = call(given, stream)
+        assert recorder.taken == [name], (i, recorder.taken)
+        monkeypatch.setattr(binding, "_native", _NoNative)
+        want, his = call(given, stream)
+        assert len(got) == len(want)
+        for j, (p, q) in enumerate(zip(got, want)):
+            assert p.dtype == q.dtype and p.shape == q.shape and torch.equal(p, q), (i, j)
+            if mine is not None:
+                assert p is mine[j] and q is his[j], (i, j)
+
+
+def test_what_the_native_part_leaves_to_python():
+    """A tensor of another layout, type or size is none that the native part takes."""
+    from paper_2607_21446_amd import binding
+    native = binding._native()
+    x = torch.zeros((8, 64), device="cuda")
+    norm = lambda x, **k: native.block_norm(x, k.get("residual"), k.get("gate"), None, None, None, None, 1, 0, 1.0, 1e-6,  # noqa: E731
+                                            k.get("h"), k.get("y"), None, k.get("stream"))
+    assert norm(x) is not None
+    for bad in (dict(x=x.t()), dict(x=x.half()), dict(x=x[0]), dict(x=x, residual=x[:4]), dict(x=x, gate=x[:3]), dict(x=x, gate=x[:0]),
+                dict(x=x, gate=x[:2, :32]), dict(x=x, y=x.bfloat16()), dict(x=x, h=x[:, :32]), dict(x=x, stream=torch.cuda.current_stream())):
+        assert norm(**bad) is None, bad
+    a, b = _codes(4, 64), _codes(6, 64)
+    linear = lambda a=a, b=b, bias=None, act=0, gate=None, res=None, out=None: native.mxfp4_linear(  # noqa: E731
+        *a, *b, bias, act, gate, res, out, None, None)
+    assert linear() is not None
+    f = torch.zeros((4, 6), device="cuda")
+    for bad in (dict(a=(a[0], a[1][:2])), dict(b=_codes(6, 32)), dict(bias=f[0, :5]), dict(gate=f[:3]), dict(act=5, b=_codes(5, 64)),
+                dict(res=f, out=f.bfloat16()), dict(out=f[:, :5]), dict(out=f[:1].expand(4, 6)), dict(gate=f[:0])):
+        assert linear(**bad) is None, bad
+    e = (b[0][None], b[1][None])
+    off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    grouped = lambda e=e, off=off, rows=None, bias=None, rs=None: native.mxfp4_grouped_linear(  # noqa: E731
+        *a, *e, off, rows, bias, 0, rs, None, None, None)
+    assert grouped() is not None
+    for bad in (dict(e=b), dict(off=off[:1]), dict(off=off.long()), dict(rows=off.long()), dict(bias=f[:2]), dict(rs=f[0, :3])):
+        assert grouped(**bad) is None, bad
