@@ -337,6 +337,7 @@ kq_status kq_block_norm_workspace_size(int64_t M, int64_t d, int64_t batches, si
  *   workspace  device, 16-byte aligned, kq_block_norm_workspace_size bytes; its
  *              contents are scratch between calls
  * dresidual may be dh and dx may be dy.  Column sums are taken in a fixed order.
+ * batches is at most 65534 (KQ_ERROR_UNSUPPORTED).
  * Enqueued on `stream`; no allocation, no synchronization.  M = 0 is a no-op (the
  * vectors' gradients are not written).
  */

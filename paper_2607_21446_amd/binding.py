@@ -9,6 +9,11 @@ the library call for plain arguments and returns None for all others (a stream
 object, a subclass, what the library refuses); those come to the checks here,
 which name what is wrong.  A calibration step with an Adam update or without a
 workspace is marshalled here.
+
+``stream`` (a torch stream or a handle) is where a call runs, torch's current stream
+if it is not given.  A workspace that a call makes for itself is that stream's; the
+results that it makes are the current stream's, so a call on another stream is ordered
+with it by the caller, or made under ``torch.cuda.stream``.
 """
 from __future__ import annotations
 

@@ -372,8 +372,8 @@ __global__ __launch_bounds__(64 * W) void mxfp4_linear_split_kernel(LinearParams
     });
 }
 
-// A few rows (a decoding step): the weight is read once and bounds the call (64 experts of 2048 x 2816 for 64 rows,
-// 196 MB: 29 us, 6.8 TB/s; one row through 3072 x 12288, 20 MB: 7.9 us, of which an empty launch is 3).  A tile is 16 TM rows of A
+// A few rows (a decoding step): the weight is read once and bounds the call (64 experts of 2048 x 2816, a row each,
+// 196 MB: 43 us, 4.5 TB/s; one row through 3072 x 12288, 20 MB: 7.2 us, of which an empty launch is 3).  A tile is 16 TM rows of A
 // by 16 of B; v_mfma_scale_f32_16x16x128_f8f6f4 takes lane l's 16 code bytes as row l % 16, block l / 16
 // of the 128-wide K step, so fragments are plain loads.  WN waves have a tile each, next to each other
 // along N, and WK waves split each tile's K, in units of 256 (whole 128-byte lines of B), D units in flight;
@@ -496,17 +496,17 @@ static int64_t rows_tiles(const LinearParams& p, int64_t bm) {
 }
 
 // Tile of a call.  Measured, us (bf16 out, weights not in the caches).
-// A few rows, K x N 3072 x 12288 / 12288 x 3072 / 1152 x 4608: tiles of 16 (32) rows and the best that splits K: 1 row
-// 7.9, 10.1, 4.4 and 10.1 (64 x 64), 15.9, 4.3 (32 x 32); 16 rows 9.6, 12.9, - and 13.6, -, -; 32 rows 15.3, 17.4, 5.2
-// and 13.5, 26.8, 4.6; 64 rows 22.5, 26.2, 6.8 (tiles of 64 rows, not kept) and 16.3, 24.6, 6.4.
-// Waves that split K, 8, 4, 2, 1: 1 row 9.2, 7.9, 9.6, 14.0; 10.1, 12.4, -, -; 8 of 64 experts of 2048 x 2816, a row each
-// 14.7, 10.7, 9.8, 12.0; all 64 56, 35.2, 29.5, 29.0; 8 experts of 2240 x 5600, 2 rows each -, 15.7, 15.5, 17.4.
-// Workgroups of 8 waves where these have 4: 1 row 9.0; 64 experts 30.6; 8 experts 16.9 us.
-// Grouped, tiles of 16 rows and 128 x 128: 64 experts of 2048 x 2816, 1, 2, 4, 8 rows an expert 29.0, 38.4, 49.2, 58.2
-// and 32.0, 38.4, 44.3, 51.6 (tiles that split K: 41.7 at 1 row); 8 experts of 2240 x 5600, 1, 2, 4, 8, 16 rows
-// 13.1, 15.5, 19.6, 23.5, 29.4 and 16.5, 20.9, 22.4, 23.6, 25.1.
-// More rows: as mxfp4_gemm's tiles; 128 x 128 and 256 x 256, grouped 32 experts 12004 x 1152 x 2240 fp32 52, 65,
-// 16 experts 16384 x 2240 x 5600 256, 219.
+// A few rows, K x N 3072 x 12288 / 12288 x 3072 / 1152 x 4608: tiles of 16 (32) rows and what splits K otherwise (64 x 64,
+// 32 x 32, 32 x 32): 1 row 7.2, 9.0, 4.2 and 10.6, 14.8, 4.0; 16 rows 9.0, 12.5, 4.5 and 11.5, 20.5, 4.2; 32 rows
+// 12.0, 16.6, 4.9 and 12.5, 25.9, 4.4; 64 rows 22.5, 26.2, 6.8 (tiles of 64 rows, not kept) and 15.3, 23.9, 6.1.
+// Waves that split K, 8, 4, 2, 1: 1 row 8.2, 7.2, 8.8, 13.0; 9.0, 11.8, 20.1, 47.0; 8 of 64 experts of 2048 x 2816, a row
+// each 13.5, 9.6, 9.0, 12.2; all 64 93, 57.1, 45.8, 43.3; 8 experts of 2240 x 5600, 2 rows each -, 17.6, 17.2, 17.4.
+// Workgroups of 8 waves where these have 4: 1 row 8.1 for 7.2; 8 tokens with 8 of 64 experts each 28.8 for 27.6.
+// Grouped, tiles of 16 rows and 128 x 128: 64 experts of 2048 x 2816, 1, 2, 4, 8 rows an expert 43.3, 44.6, 47.1, 51.0
+// and 51.2, 48.0, 49.3, 50.8 (tiles that split K: 66.6 at 1 row); 8 experts of 2240 x 5600, 1, 2, 4, 8, 16 rows
+// 17.2, 17.2, 17.5, 17.8, 20.0 and 21.9, 21.9, 22.1, 22.2, 22.7: the rule's 2 and 8 rows are below where the two meet.
+// More rows: as mxfp4_gemm's tiles; 128 x 128 and 256 x 256, grouped 32 experts 12004 x 1152 x 2240 fp32 61, 76,
+// 16 experts 16384 x 2240 x 5600 224, 203.
 enum class LinearTile { Rows16, Rows32, Split32, Split64, Pipe128, Pipe256 };
 
 static LinearTile linear_tile_of(const LinearParams& p) {
