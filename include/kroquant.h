@@ -349,6 +349,131 @@ kq_status kq_block_norm_backward(const void* dy, const void* dh, const void* x, 
                                  float* dshift, float* dweight, float* dpost_weight, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/* Type of the positions that kq_rope takes, and which two elements of a row a pair is. */
+typedef enum kq_position { KQ_POSITION_INT32 = 0, KQ_POSITION_INT64 = 1, KQ_POSITION_FP32 = 2 } kq_position;
+typedef enum kq_pairing {
+    KQ_PAIRING_PAIRS = 0, /* pair p: elements 2p and 2p + 1                       */
+    KQ_PAIRING_HALVES = 1 /* pair p: elements p and p + n, n pairs in all          */
+} kq_pairing;
+
+/*
+ * kq_rope -- rotary positions with one to four axes (a text's; an image's row
+ * and column; a video's time, row and column), and their gradient.  The first
+ * 2n of a row's D elements, n = sum(axes) / 2, are n pairs; the first axes[0] / 2
+ * of them turn with the first position of the token, the next axes[1] / 2 with
+ * its second, and so on:
+ *     y_a = x_a cos w - x_b sin w,  y_b = x_b cos w + x_a sin w,
+ *     w = position f,  f = theta^(-2i / axes[j]) for pair i of section j
+ * (KQ_PAIRING_HALVES takes the pairs' order over all sections).  The other
+ * D - 2n elements go through.  backward = 1: w is -w, the gradient of x from
+ * that of y.
+ *   x, y       [T, H, D] of dtype, element (t, h, 0) at t * x_token + h * x_head
+ *              elements (y alike); strides are >= 0, y's rows do not overlap.  y
+ *              may be x itself with the same strides, and overlaps x in no other way
+ *   positions  [T, n_axes] of pos_type, row t at t * pos_stride elements
+ *   axes       HOST int [n_axes], each a positive even number
+ *   theta      > 0; not used with freqs
+ *   freqs      device fp64 [n] or NULL: the pairs' f, in radians a position
+ * Angles are in 64 bits, the rotation in 32 with one rounding.  D is even, 2 to
+ * 1024; H at most 65535.  Arrays are aligned to their elements.  T, H = 0 is a
+ * no-op.  Enqueued on `stream`; no allocation, no synchronization.
+ */
+kq_status kq_rope(const void* x, kq_dtype dtype, int64_t T, int64_t H, int64_t D, int64_t x_token, int64_t x_head,
+                  const void* positions, kq_position pos_type, int64_t pos_stride, const int* axes, int n_axes,
+                  double theta, const double* freqs, kq_pairing pairing, int backward, void* y, int64_t y_token,
+                  int64_t y_head, void* stream);
+
+/* What a cache's elements are: bf16; or blocks of 32 along a row with an E8M0 scale (OCP Microscaling v1.0). */
+typedef enum kq_cache_format {
+    KQ_CACHE_BF16 = 0,
+    KQ_CACHE_MXFP8 = 1, /* E4M3: s = max(floor(log2 amax) - 8 + 127, 0), saturating at 448         */
+    KQ_CACHE_MXFP4 = 2  /* E2M1 as everywhere in this library: two to a byte, saturating at 6     */
+} kq_cache_format;
+
+/*
+ * A paged cache of keys and values (a HOST struct of device pointers; the caller
+ * owns the arrays).  k and v are [pages, heads, page_size, row] with rows of d
+ * bf16, d bytes (MXFP8) or d / 2 bytes (MXFP4), 16-byte aligned; the scales are
+ * [pages, heads, page_size, d / 32] (NULL for bf16).  page_size is a power of two
+ * from 16 to 32768, d a multiple of 32 up to 256, heads 1 to 65535.  Slot i is
+ * token i % page_size of page i / page_size.
+ */
+typedef struct kq_kv_cache {
+    void* k;
+    void* v;
+    uint8_t* k_scales;
+    uint8_t* v_scales;
+    kq_cache_format format;
+    int64_t pages, heads, page_size, d;
+} kq_kv_cache;
+
+/*
+ * kq_kv_cache_write -- tokens' keys and values into their slots, quantized on the
+ * way (rounded to nearest, ties to even).
+ *   k, v   [T, heads, d] of dtype, element (t, h, 0) at t * k_token + h * k_head
+ *   slots  device int64 [T].  A token whose slot is outside the cache is left
+ *          out.  A slot given twice holds eights of columns of either token.
+ * As for the quantizers, inputs must be finite.  Arrays are aligned to their
+ * elements.  T = 0 is a no-op.  Enqueued on `stream`; no allocation, no
+ * synchronization.
+ */
+kq_status kq_kv_cache_write(const kq_kv_cache* cache, const void* k, const void* v, kq_dtype dtype, int64_t T, int64_t k_token,
+                            int64_t k_head, int64_t v_token, int64_t v_head, const int64_t* slots, void* stream);
+
+/*
+ * kq_kv_cache_read -- the values that slots hold, of dtype: k, v [T, heads, d],
+ * contiguous, 16-byte aligned.  Rows of slots outside the cache are zeros.
+ * Values are exact, but for those below 2^-126, which may come as zero.
+ */
+kq_status kq_kv_cache_read(const kq_kv_cache* cache, const int64_t* slots, int64_t T, void* k, void* v, kq_dtype dtype, void* stream);
+
+/* Bytes of device workspace that kq_paged_attention needs for B sequences and q_heads query heads on this cache. */
+kq_status kq_paged_attention_workspace_size(int64_t B, int64_t q_heads, int64_t heads, int64_t d, size_t* bytes);
+
+/*
+ * kq_paged_attention -- attention of one new token of every sequence over a cache:
+ *     out[b, i] = softmax(scale q[b, i] K^T) V
+ * with K and V the rows of head i / (q_heads / heads) of sequence b's tokens
+ * max(0, n - window) .. n - 1, n = lengths[b] (the new token's own key and value are
+ * written before).  A sequence without tokens gives zeros and lse = -infinity.
+ *   q, out      [B, q_heads, d] of dtype, element (b, i, 0) at b * q_seq + i * q_head
+ *               elements; q_heads a multiple of the cache's heads; out may be q itself
+ *               with the same strides
+ *   page_table  device int32 [B, max_pages], row b at b * table_stride: the pages of a
+ *               sequence in order.  Entries past a sequence's last page are not read.
+ *   lengths     device int32 [B].  (Nothing outside the arrays is touched for pages
+ *               outside the cache or lengths outside 0 .. max_pages * page_size: they
+ *               are taken as the nearest ones inside.)
+ *   window      0: all tokens count
+ *   lse         device fp32 [B, q_heads] or NULL: log(sum(exp(scores))), to join results
+ *   workspace   device, 16-byte aligned, kq_paged_attention_workspace_size bytes; its
+ *               contents are scratch between calls
+ * What the cache holds behind a sequence's tokens or before its window does not matter
+ * (NaN among it).  Sums are in 32 bits and in a fixed order for given lengths.  B is at
+ * most 2^20, q_heads 65535, a sequence's tokens 2^31 - 64.  B = 0 is a no-op.  Enqueued on
+ * `stream`; no allocation, no synchronization.
+ */
+kq_status kq_paged_attention(const void* q, kq_dtype dtype, int64_t B, int64_t q_heads, int64_t q_seq, int64_t q_head,
+                             const kq_kv_cache* cache, const int32_t* page_table, int64_t table_stride, int64_t max_pages,
+                             const int32_t* lengths, float scale, int64_t window, void* out, int64_t out_seq,
+                             int64_t out_head, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * kq_w4a16_linear -- kq_mxfp4_linear for a few rows whose activations are not
+ * quantized (a decoding loop's):
+ *     out = residual + gate act(x deq(B)^T + bias)
+ *   x        [M, K] of x_dtype, row stride ldx >= K elements
+ *   others   as for kq_mxfp4_linear
+ * The weight is read once for each 16 rows.  Products of bf16 values are exact, x in
+ * 32 bits takes part in full (finite values only); sums are in 32 bits, in a fixed
+ * order.  M is at most 65535 * 16.  M, N = 0 is a no-op.  Enqueued on `stream`; no
+ * allocation, no synchronization.
+ */
+kq_status kq_w4a16_linear(const void* x, kq_dtype x_dtype, int64_t M, int64_t ldx, const uint8_t* b_codes,
+                          const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
+                          int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act, const void* residual,
+                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream);
+
 /*
  * kq_mxfp4_quantize -- the bare MXFP4 quantizer ("Q4", the lower bound of
  * Sec. 4.4): y = x, then MXFP4.

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkroquant.so")
 BIND = os.path.join(PKG, "_kqbind.so")  # native marshalling of the Python binding
-SOURCES = ["kq_kernels.hip", "kq_gemm.hip", "kq_linear.hip", "kq_norm.hip", "kq_calib.hip", "kq_api.hip"]
+SOURCES = ["kq_kernels.hip", "kq_gemm.hip", "kq_linear.hip", "kq_norm.hip", "kq_rope.hip", "kq_cache.hip", "kq_attn.hip", "kq_matvec.hip",
+           "kq_calib.hip", "kq_api.hip"]
 
 # -packed-fp32-ops off: no v_pk_{add,mul,fma}_f32 in the device code.
 # -ffp-contract=off: only the explicit fmaf calls fuse, which keeps the

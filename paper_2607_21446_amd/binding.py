@@ -21,6 +21,7 @@ import contextlib
 import ctypes
 import os
 from functools import lru_cache
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -41,6 +42,8 @@ EXPORTED = (
     "kq_calib_step_noalloc",
     "kq_mxfp4_linear", "kq_mxfp4_grouped_linear", "kq_block_norm", "kq_block_norm_workspace_size",
     "kq_block_norm_backward",
+    "kq_rope", "kq_kv_cache_write", "kq_kv_cache_read", "kq_paged_attention_workspace_size", "kq_paged_attention",
+    "kq_w4a16_linear",
     "kq_status_string", "kq_last_error_detail", "kq_version",
 )
 
@@ -51,6 +54,12 @@ class KQError(RuntimeError):
         self.name = STATUS.get(status, f"status {status}")
         self.detail = detail
         super().__init__(f"{call}: {self.name}: {detail}")
+
+
+class _CacheStruct(ctypes.Structure):  # kq_kv_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("format", ctypes.c_int), ("pages", ctypes.c_int64), ("heads", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("d", ctypes.c_int64)]
 
 
 @lru_cache(maxsize=1)
@@ -90,6 +99,13 @@ def lib() -> ctypes.CDLL:
     L.kq_block_norm_workspace_size.argtypes = [I64, I64, I64, ctypes.POINTER(ctypes.c_size_t)]
     L.kq_block_norm_backward.argtypes = [P, P, P, I, P, I, I64, I64, I64, P, I64, P, I64, P, P, I, I, I, F, F, P, P, P, P,
                                          P, P, P, P, ctypes.c_size_t, P]
+    D, IP, C = ctypes.c_double, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(_CacheStruct)
+    L.kq_rope.argtypes = [P, I, I64, I64, I64, I64, I64, P, I, I64, IP, I, D, P, I, I, P, I64, I64, P]
+    L.kq_kv_cache_write.argtypes = [C, P, P, I, I64, I64, I64, I64, I64, P, P]
+    L.kq_kv_cache_read.argtypes = [C, P, I64, P, P, I, P]
+    L.kq_paged_attention_workspace_size.argtypes = [I64, I64, I64, I64, ctypes.POINTER(ctypes.c_size_t)]
+    L.kq_paged_attention.argtypes = [P, I, I64, I64, I64, I64, C, P, I64, I64, P, F, I64, P, I64, I64, P, P, ctypes.c_size_t, P]
+    L.kq_w4a16_linear.argtypes = [P, I, I64, I64, P, P, I64, I64, P, P, I64, I64, I, I, P, I64, P, I64, I, P]
     for name in EXPORTED[:-3]:
         getattr(L, name).restype = ctypes.c_int
     L.kq_status_string.argtypes = [I]
@@ -629,6 +645,305 @@ def block_norm_backward(dy, h, dh=None, x=None, gate=None, post_weight=None, wei
             *(_ptr(out.get(n)) for n in ("dgate", "dscale", "dshift", "dweight", "dpost_weight")), _ptr(workspace),
             workspace.numel(), _stream(stream)), "kq_block_norm_backward")
     return {"dx": dresidual if dx is None else dx, "dresidual": dresidual, **out}
+
+
+# ------------------------------------------------------------ a generation step
+
+_POSITIONS = {torch.int32: 0, torch.int64: 1, torch.float32: 2}  # kq_position
+_PAIRINGS = {"pairs": 0, "halves": 1}  # kq_pairing
+_FORMATS = {"bf16": 0, "mxfp8": 1, "mxfp4": 2}  # kq_cache_format
+
+
+def _at(device, stream):
+    """The call's stream, with ``device`` current: torch's current stream is that device's."""
+    return torch.cuda.device(device), _stream(stream) if stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _heads_of(t, name, shape=None, device=None, dtype=None, written=False):
+    """A [rows, heads, columns] array whose columns are contiguous: its two strides."""
+    _float(t, name, dtype)
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)) or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be {'[rows, heads, columns]' if shape is None else list(shape)}"
+                         f"{'' if device is None else f' on {device}'}, got {list(t.shape)} on {t.device}")
+    T, H, D = t.shape
+    if D > 1 and t.stride(2) != 1:
+        raise ValueError(f"the columns of {name} must be contiguous")
+    a, b = t.stride(0) if T > 1 else H * D, t.stride(1) if H > 1 else D
+    if written:
+        reach = D
+        for stride, n in sorted([(a, T), (b, H)]):
+            if n > 1 and stride < reach:
+                raise ValueError(f"the rows of {name} overlap")
+            reach += stride * (n - 1) if n > 1 else 0
+    return a, b
+
+
+def _overlap(a, b):
+    """Whether two arrays of one layout share memory without being the same."""
+    if a.data_ptr() == b.data_ptr() and a.stride() == b.stride():
+        return False
+    if not a.numel() or not b.numel():
+        return False
+    end = lambda t: t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))  # noqa: E731
+    return a.data_ptr() < end(b) and b.data_ptr() < end(a)
+
+
+def _rope(name, x, positions, axes, theta, pairing, freqs, backward, out, out_name, stream):
+    pair = _one_of(_PAIRINGS, pairing, "pairing")
+    r = _native().rope(x, positions, axes, theta, pair, freqs, backward, out, stream)
+    if r is not None:
+        return r
+    xs = _heads_of(x, name)
+    axes = tuple(int(a) for a in ((axes,) if isinstance(axes, int) else axes))
+    T, H, D = x.shape
+    if positions.dtype not in _POSITIONS:
+        raise TypeError(f"positions must be int32, int64 or float32, got {positions.dtype}")
+    if positions.device != x.device:
+        raise ValueError(f"positions are on {positions.device}, {name} on {x.device}")
+    if positions.dim() == 1 and len(axes) == 1:
+        positions = positions.unsqueeze(1)
+    if tuple(positions.shape) != (T, len(axes)) or (len(axes) > 1 and positions.stride(1) != 1):
+        raise ValueError(f"positions must be [{T}, {len(axes)}] with contiguous rows, got {list(positions.shape)}")
+    if freqs is not None:
+        _need(freqs, torch.float64, "freqs")
+        _size(freqs, sum(axes) // 2, "freqs", x.device)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+    os_ = _heads_of(out, out_name, x.shape, x.device, x.dtype, written=True)
+    if _overlap(x, out):
+        raise ValueError(f"{out_name} overlaps {name} without being it")
+    guard, st = _at(x.device, stream)
+    with guard:
+        _check(lib().kq_rope(_ptr(x), _FLOATS[x.dtype], T, H, D, *xs, _ptr(positions), _POSITIONS[positions.dtype],
+                             positions.stride(0) if T > 1 else len(axes), (ctypes.c_int * len(axes))(*axes), len(axes), float(theta),
+                             _ptr(freqs), pair, int(backward), _ptr(out), *os_, st), "kq_rope")
+    return out
+
+
+def rope(x, positions, axes, theta=10000.0, pairing="pairs", freqs=None, out=None, stream=None):
+    """kq_rope: rotary positions with one to four axes.  x [T, H, D] fp32 or bf16 (rows
+    of columns side by side at any strides: heads of a fused projection); positions
+    [T, len(axes)] (or [T] for one axis) int32, int64 or float32; ``axes`` how many
+    elements of a row turn with each, in order (the rest go through).  ``pairing``:
+    "pairs" (2p, 2p + 1) or "halves" (p, p + n).  Pair i of an axis of a elements turns
+    by position * theta^(-2i / a), or pair p by position * freqs[p] (device fp64, one
+    for each pair).  out may be x.  Returns out."""
+    return _rope("x", x, positions, axes, theta, pairing, freqs, False, out, "out", stream)
+
+
+def rope_backward(dy, positions, axes, theta=10000.0, pairing="pairs", freqs=None, dx=None, stream=None):
+    """kq_rope with backward = 1: the gradient of rope's x from that of its result.
+    Arguments as rope's; dx may be dy.  Returns dx."""
+    return _rope("dy", dy, positions, axes, theta, pairing, freqs, True, dx, "dx", stream)
+
+
+class KVCache(NamedTuple):
+    """A paged cache: k and v [pages, heads, page_size, row] with rows of d bf16, d bytes
+    (MXFP8) or d / 2 bytes (MXFP4), and uint8 scales [pages, heads, page_size, d / 32]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: Optional[torch.Tensor] = None
+    v_scales: Optional[torch.Tensor] = None
+
+    @property
+    def d(self):
+        return self.k.shape[-1] if self.k_scales is None else 32 * self.k_scales.shape[-1]
+
+    @property
+    def format(self):
+        if self.k_scales is None:
+            return "bf16"
+        return "mxfp8" if self.k.shape[-1] == self.d else "mxfp4"
+
+    @property
+    def page_size(self):
+        return self.k.shape[-2]
+
+
+def kv_cache(pages, page_size, heads, d, format="mxfp4", device="cuda"):
+    """A paged cache of zeros: ``format`` "bf16", "mxfp8" or "mxfp4", page_size a power of
+    two from 16 to 32768, d a multiple of 32 up to 256."""
+    f = _one_of(_FORMATS, format, "format")
+    if d < 32 or d % 32 or d > 256 or page_size < 16 or page_size > 32768 or page_size & (page_size - 1) or pages < 1 or heads < 1:
+        raise ValueError(f"no cache of {pages} pages of {page_size} tokens, {heads} heads of {d}: page_size must be a power of two "
+                         "in [16, 32768], d a multiple of 32 in [32, 256]")
+    make = lambda n, t: torch.zeros((pages, heads, page_size, n), dtype=t, device=device)  # noqa: E731
+    if f == 0:
+        return KVCache(make(d, torch.bfloat16), make(d, torch.bfloat16))
+    row = d if f == 1 else d // 2
+    return KVCache(*(make(n, torch.uint8) for n in (row, row, d // 32, d // 32)))
+
+
+def _cache(cache):
+    """kq_kv_cache of a KVCache."""
+    if not isinstance(cache, KVCache):
+        raise TypeError(f"cache must be a KVCache, got {type(cache).__name__}")
+    scaled = cache.k_scales is not None
+    for name in ("k", "v") + (("k_scales", "v_scales") if scaled else ()):
+        t = getattr(cache, name)
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"the cache's {name} must be a tensor")
+        _need(t, torch.uint8 if scaled else torch.bfloat16, f"the cache's {name}")
+        like = cache.k if name == "v" else cache.k_scales if name == "v_scales" else None
+        if t.dim() != 4 or t.device != cache.k.device or (like is not None and t.shape != like.shape):
+            raise ValueError(f"the cache's {name} must be [pages, heads, page_size, row] as the others, got {list(t.shape)} on {t.device}")
+    if scaled and (cache.k_scales.shape[:3] != cache.k.shape[:3] or cache.k.shape[3] not in (cache.d, cache.d // 2)):
+        raise ValueError(f"rows of {cache.k.shape[3]} bytes do not go with {cache.k_scales.shape[3]} scales")
+    if not scaled and cache.v_scales is not None:
+        raise ValueError("a bf16 cache has no scales")
+    pages, heads, size, _ = cache.k.shape
+    return _CacheStruct(_ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scales), _ptr(cache.v_scales), _FORMATS[cache.format], pages,
+                        heads, size, cache.d)
+
+
+def _slots(slots, device):
+    _need(slots, torch.int64, "slots")
+    if slots.dim() != 1 or slots.device != device:
+        raise ValueError(f"slots must be one-dimensional on {device}, got {list(slots.shape)} on {slots.device}")
+    return slots.numel()
+
+
+def kv_cache_write(cache, k, v, slots, stream=None):
+    """kq_kv_cache_write: tokens' keys and values k, v [T, heads, d] (fp32 or bf16, of one
+    type, columns contiguous) into the slots (int64 [T], page * page_size + token in the
+    page; a token whose slot is outside the cache is left out; a slot comes once), rounded
+    to the cache's format.  Returns cache."""
+    r = _native().kv_cache_write(cache, k, v, slots, stream)
+    if r is not None:
+        return r
+    c = _cache(cache)
+    dev = cache.k.device
+    T = _slots(slots, dev)
+    ks = _heads_of(k, "k", (T, c.heads, c.d), dev)
+    vs = _heads_of(v, "v", (T, c.heads, c.d), dev, k.dtype)
+    guard, st = _at(dev, stream)
+    with guard:
+        _check(lib().kq_kv_cache_write(ctypes.byref(c), _ptr(k), _ptr(v), _FLOATS[k.dtype], T, *ks, *vs, _ptr(slots), st),
+               "kq_kv_cache_write")
+    return cache
+
+
+def kv_cache_read(cache, slots, k=None, v=None, out_dtype=None, stream=None):
+    """kq_kv_cache_read: the keys and values that slots (int64 [T]) hold, zeros for slots
+    outside the cache.  Returns (k, v), [T, heads, d] bf16 unless ``out_dtype`` says fp32."""
+    r = _native().kv_cache_read(cache, slots, k, v, out_dtype, stream)
+    if r is not None:
+        return r
+    c = _cache(cache)
+    dev = cache.k.device
+    T = _slots(slots, dev)
+    shape = (T, c.heads, c.d)
+    given = next((t for t in (k, v) if t is not None), None)
+    dtype = out_dtype or (torch.bfloat16 if given is None else given.dtype)
+    k, v = (torch.empty(shape, dtype=dtype, device=dev) if t is None else t for t in (k, v))
+    for t, name in ((k, "k"), (v, "v")):
+        _float(t, name, dtype)
+        if tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {list(shape)} on {dev}, got {list(t.shape)} on {t.device}")
+    guard, st = _at(dev, stream)
+    with guard:
+        _check(lib().kq_kv_cache_read(ctypes.byref(c), _ptr(slots), T, _ptr(k), _ptr(v), _FLOATS[dtype], st), "kq_kv_cache_read")
+    return k, v
+
+
+def paged_attention_workspace(B, q_heads, heads, d, device="cuda"):
+    """Device workspace of paged_attention for B sequences, q_heads query heads and a cache's heads of d."""
+    n = ctypes.c_size_t(0)
+    _check(lib().kq_paged_attention_workspace_size(B, q_heads, heads, d, ctypes.byref(n)), "kq_paged_attention_workspace_size")
+    return torch.empty(int(n.value), dtype=torch.uint8, device=device)
+
+
+def paged_attention(q, cache, page_table, lengths, scale=None, window=None, out=None, lse=None, want_lse=False, workspace=None,
+                    stream=None):
+    """kq_paged_attention: softmax(scale q K^T) V of one new token of every sequence, q
+    [B, q_heads, d] fp32 or bf16 (columns contiguous), over the tokens of ``cache``
+    that page_table (int32 [B, max_pages], rows contiguous) and lengths (int32 [B])
+    name, or the last ``window`` of them.  Query heads i * group .. (i + 1) * group - 1
+    share the cache's head i.  ``scale``: 1 / sqrt(d) if not given.  An empty sequence
+    gives zeros.  Returns out (of q's type), or with ``want_lse`` or an ``lse``
+    (out, lse): fp32 [B, q_heads], the logarithm of the sum of exponentials (-inf for
+    an empty sequence).  Two calls that may run at once need a ``workspace`` each, two
+    captured graphs that are replayed at once too."""
+    r = _native().paged_attention(q, cache, page_table, lengths, scale, window, out, lse, want_lse, workspace, stream)
+    if r is not None:
+        return r
+    c = _cache(cache)
+    dev = cache.k.device
+    qs = _heads_of(q, "q", device=dev)
+    B, Hq, d = q.shape
+    if d != c.d or Hq < 1 or Hq % c.heads:
+        raise ValueError(f"q must be [B, a multiple of {c.heads}, {c.d}], got {list(q.shape)}")
+    for t, name, dims in ((page_table, "page_table", 2), (lengths, "lengths", 1)):
+        if t.dtype != torch.int32:
+            raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
+        if t.device != dev or t.dim() != dims or t.shape[0] != B or (t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name} must be [{B}{', max_pages' if dims == 2 else ''}] with contiguous rows on {dev}, "
+                             f"got {list(t.shape)} on {t.device}")
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least 1, got {window}")
+    if out is None:
+        out = torch.empty((B, Hq, d), dtype=q.dtype, device=dev)
+    os_ = _heads_of(out, "out", (B, Hq, d), dev, q.dtype, written=True)
+    if _overlap(q, out):
+        raise ValueError("out overlaps q without being it")
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+    if lse is not None:
+        _need(lse, torch.float32, "lse")
+        _size(lse, B * Hq, "lse", dev)
+    if workspace is None:
+        with torch.cuda.device(dev), _scratch_of(stream, dev):
+            workspace = paged_attention_workspace(B, Hq, c.heads, c.d, dev)
+    _need(workspace, torch.uint8, "workspace")
+    if workspace.device != dev:
+        raise ValueError(f"workspace is on {workspace.device}, the cache on {dev}")
+    guard, st = _at(dev, stream)
+    with guard:
+        _check(lib().kq_paged_attention(_ptr(q), _FLOATS[q.dtype], B, Hq, *qs, ctypes.byref(c), _ptr(page_table),
+                                        page_table.stride(0) if B > 1 else page_table.shape[1], page_table.shape[1], _ptr(lengths),
+                                        d ** -0.5 if scale is None else float(scale), window or 0, _ptr(out), *os_, _ptr(lse),
+                                        _ptr(workspace), workspace.numel(), st), "kq_paged_attention")
+    return out if lse is None else (out, lse)
+
+
+def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=None, out=None, out_dtype=None, stream=None):
+    """kq_w4a16_linear: out = residual + gate * act(x deq(B)^T + bias) for a few rows x
+    [M, K] of fp32 or bf16 that are not quantized (a decoding loop's) and an MXFP4
+    weight b_codes [N, K/2], b_scales [N, K/32].  The other arguments are
+    mxfp4_linear's.  Returns out."""
+    a = _one_of(_ACTS, act, "act")
+    r = _native().w4a16_linear(x, b_codes, b_scales, bias, a, gate, residual, out, out_dtype, stream)
+    if r is not None:
+        return r
+    for t, name in ((b_codes, "b_codes"), (b_scales, "b_scales")):
+        _need(t, torch.uint8, name)
+    _float(x, "x")
+    M, K = _matrix(x, "x")
+    N = _matrix(b_codes, "b_codes")[0]
+    dev = x.device
+    if b_codes.shape[1] * 2 != K or tuple(b_scales.shape) != (N, K // 32):
+        raise ValueError("operand shapes do not match")
+    if b_codes.device != dev or b_scales.device != dev:
+        raise ValueError("all operands must be on one device")
+    ldx = _rows_of(x, (M, K), "x", dev)
+    if act == "swiglu" and N % 2:
+        raise ValueError(f"swiglu needs an even number of columns, got {N}")
+    cols = N // 2 if act == "swiglu" else N
+    vec = _vectors([("bias", bias, False)], N, dev)[0]
+    gvec, B, strides = _vectors([("gate", gate, True)], cols, dev)
+    if bias is not None and gate is not None and vec != gvec:
+        raise TypeError(f"bias and gate must have one type, got {bias.dtype} and {gate.dtype}")
+    _batches(M, B)
+    if out is None and out_dtype is None and residual is not None:
+        out_dtype = residual.dtype
+    out, ldo = _linear_out(out, M, cols, out_dtype, dev)
+    ldr = 0 if residual is None else _rows_of(residual, (M, cols), "residual", dev, out.dtype)
+    guard, st = _at(dev, stream)
+    with guard:
+        _check(lib().kq_w4a16_linear(_ptr(x), _FLOATS[x.dtype], M, ldx, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(bias), _ptr(gate),
+                                     strides[0], max(1, M // B), vec if gate is None else gvec, a, _ptr(residual), ldr, _ptr(out), ldo,
+                                     _FLOATS[out.dtype], st), "kq_w4a16_linear")
+    return out
 
 
 def mxfp4(X, codes=None, scales=None, stream=None):

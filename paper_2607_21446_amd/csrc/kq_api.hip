@@ -17,6 +17,7 @@
 #include "kq_kernels.h"
 #include "kq_linear.h"
 #include "kq_norm.h"
+#include "kq_serve.h"
 #include "kroquant.h"
 
 namespace {
@@ -597,6 +598,228 @@ kq_status kq_block_norm_backward(const void* dy, const void* dh, const void* x, 
     p.dpost_weight = dpost_weight;
     p.partial = static_cast<float*>(workspace);
     return from_hip(kq::launch_block_norm_backward(p, (hipStream_t)stream), "kq_block_norm_backward");
+}
+
+kq_status kq_rope(const void* x, kq_dtype dtype, int64_t T, int64_t H, int64_t D, int64_t x_token, int64_t x_head,
+                  const void* positions, kq_position pos_type, int64_t pos_stride, const int* axes, int n_axes,
+                  double theta, const double* freqs, kq_pairing pairing, int backward, void* y, int64_t y_token,
+                  int64_t y_head, void* stream) {
+    if (T < 0 || T > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "T = %lld must be in [0, 2^31 - 1]", (long long)T);
+    if (H < 0 || H > 65535) return fail(KQ_ERROR_INVALID_VALUE, "H = %lld must be in [0, 65535]", (long long)H);
+    if (D < 2 || D % 2 || D > kq::kRopeMaxColumns)
+        return fail(KQ_ERROR_INVALID_VALUE, "D = %lld must be even and in [2, %lld]", (long long)D, (long long)kq::kRopeMaxColumns);
+    if (!dtype_ok(dtype)) return fail(KQ_ERROR_INVALID_VALUE, "dtype = %d must be a kq_dtype", (int)dtype);
+    if (pos_type < KQ_POSITION_INT32 || pos_type > KQ_POSITION_FP32)
+        return fail(KQ_ERROR_INVALID_VALUE, "pos_type = %d must be a kq_position", (int)pos_type);
+    if (pairing != KQ_PAIRING_PAIRS && pairing != KQ_PAIRING_HALVES)
+        return fail(KQ_ERROR_INVALID_VALUE, "pairing = %d must be a kq_pairing", (int)pairing);
+    if (backward != 0 && backward != 1) return fail(KQ_ERROR_INVALID_VALUE, "backward = %d must be 0 or 1", backward);
+    if (n_axes < 1 || n_axes > kq::kRopeMaxAxes)
+        return fail(KQ_ERROR_INVALID_VALUE, "n_axes = %d must be in [1, %d]", n_axes, kq::kRopeMaxAxes);
+    if (!axes) return fail(KQ_ERROR_NULL_POINTER, "axes must not be NULL");
+    kq::RopeParams p{};
+    int64_t sum = 0;
+    for (int i = 0; i < n_axes; ++i) {
+        if (axes[i] < 2 || axes[i] % 2) return fail(KQ_ERROR_INVALID_VALUE, "axes[%d] = %d must be positive and even", i, axes[i]);
+        sum += axes[i];
+        if (sum > D) return fail(KQ_ERROR_INVALID_VALUE, "the axes have more than D = %lld elements", (long long)D);
+        p.end[i] = (int)(sum / 2);
+    }
+    if (!freqs && !(theta > 0.0 && theta <= 1e300)) return fail(KQ_ERROR_INVALID_VALUE, "theta must be positive and finite");
+    if (x_token < 0 || x_head < 0 || y_token < 0 || y_head < 0 || pos_stride < 0)
+        return fail(KQ_ERROR_INVALID_VALUE, "strides must be >= 0");
+    if ((T > 1 && y_token < D) || (H > 1 && y_head < D)) return fail(KQ_ERROR_INVALID_VALUE, "the rows of y overlap");
+    if (T == 0 || H == 0) return ok();
+    if (!x || !y || !positions) return fail(KQ_ERROR_NULL_POINTER, "x, positions and y must not be NULL");
+    if (!aligned(x, dtype_bytes(dtype)) || !aligned(y, dtype_bytes(dtype)) || !aligned(freqs, 8) ||
+        !aligned(positions, pos_type == KQ_POSITION_INT64 ? 8 : 4))
+        return fail(KQ_ERROR_MISALIGNED, "x, positions, freqs and y must be aligned to their elements");
+    p.x = x;
+    p.y = y;
+    p.T = T;
+    p.H = (int)H;
+    p.D = (int)D;
+    p.x_token = x_token;
+    p.x_head = x_head;
+    p.y_token = y_token;
+    p.y_head = y_head;
+    p.positions = positions;
+    p.pos_stride = pos_stride;
+    p.pos_type = static_cast<kq::Position>(pos_type);
+    p.axes = n_axes;
+    p.log2_theta = freqs ? 0.0 : std::log2(theta);
+    p.freqs = freqs;
+    p.halves = pairing == KQ_PAIRING_HALVES;
+    p.is16 = dtype == KQ_DTYPE_BF16;
+    p.backward = backward;
+    return from_hip(kq::launch_rope(p, (hipStream_t)stream), "kq_rope");
+}
+
+// Sizes and, where `arrays`, pointers of a cache.
+static kq_status check_cache(const kq_kv_cache* c, bool arrays, kq::Cache* out) {
+    if (!c) return fail(KQ_ERROR_NULL_POINTER, "cache must not be NULL");
+    if (c->format < KQ_CACHE_BF16 || c->format > KQ_CACHE_MXFP4)
+        return fail(KQ_ERROR_INVALID_VALUE, "format = %d must be a kq_cache_format", (int)c->format);
+    if (c->d < 32 || c->d % 32 || c->d > kq::kCacheMaxColumns)
+        return fail(KQ_ERROR_INVALID_VALUE, "d = %lld must be a multiple of 32 in [32, %lld]", (long long)c->d, (long long)kq::kCacheMaxColumns);
+    if (c->heads < 1 || c->heads > 65535) return fail(KQ_ERROR_INVALID_VALUE, "heads = %lld must be in [1, 65535]", (long long)c->heads);
+    if (c->page_size < 16 || c->page_size > 32768 || (c->page_size & (c->page_size - 1)))
+        return fail(KQ_ERROR_INVALID_VALUE, "page_size = %lld must be a power of two in [16, 32768]", (long long)c->page_size);
+    if (c->pages < 1 || c->pages > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "pages = %lld must be in [1, 2^31 - 1]", (long long)c->pages);
+    if (c->pages > (INT64_MAX >> 2) / (c->heads * c->page_size * c->d))
+        return fail(KQ_ERROR_INVALID_VALUE, "the cache of %lld pages is too large", (long long)c->pages);
+    if (!arrays) return ok();
+    if (!c->k || !c->v) return fail(KQ_ERROR_NULL_POINTER, "the cache's k and v must not be NULL");
+    if (c->format != KQ_CACHE_BF16 && (!c->k_scales || !c->v_scales))
+        return fail(KQ_ERROR_NULL_POINTER, "a quantized cache's scales must not be NULL");
+    if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(KQ_ERROR_MISALIGNED, "the cache's k and v must be 16-byte aligned");
+    out->k = static_cast<uint8_t*>(c->k);
+    out->v = static_cast<uint8_t*>(c->v);
+    out->k_scales = c->k_scales;
+    out->v_scales = c->v_scales;
+    out->format = static_cast<kq::CacheFormat>(c->format);
+    out->pages = c->pages;
+    out->heads = (int)c->heads;
+    out->page_size = (int)c->page_size;
+    out->d = (int)c->d;
+    out->page_shift = 0;
+    while ((int64_t(1) << out->page_shift) < c->page_size) ++out->page_shift;
+    return ok();
+}
+
+kq_status kq_kv_cache_write(const kq_kv_cache* cache, const void* k, const void* v, kq_dtype dtype, int64_t T, int64_t k_token,
+                            int64_t k_head, int64_t v_token, int64_t v_head, const int64_t* slots, void* stream) {
+    if (T < 0 || T > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "T = %lld must be in [0, 2^31 - 1]", (long long)T);
+    if (!dtype_ok(dtype)) return fail(KQ_ERROR_INVALID_VALUE, "dtype = %d must be a kq_dtype", (int)dtype);
+    if (k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return fail(KQ_ERROR_INVALID_VALUE, "strides must be >= 0");
+    kq::CacheCopyParams p{};
+    const kq_status st = check_cache(cache, T > 0, &p.c);
+    if (st != KQ_SUCCESS || T == 0) return st;
+    if (!k || !v || !slots) return fail(KQ_ERROR_NULL_POINTER, "k, v and slots must not be NULL");
+    if (!aligned(k, dtype_bytes(dtype)) || !aligned(v, dtype_bytes(dtype)) || !aligned(slots, 8))
+        return fail(KQ_ERROR_MISALIGNED, "k, v and slots must be aligned to their elements");
+    p.slots = slots;
+    p.T = T;
+    p.k = const_cast<void*>(k);
+    p.v = const_cast<void*>(v);
+    p.k_token = k_token;
+    p.k_head = k_head;
+    p.v_token = v_token;
+    p.v_head = v_head;
+    p.is16 = dtype == KQ_DTYPE_BF16;
+    return from_hip(kq::launch_cache_write(p, (hipStream_t)stream), "kq_kv_cache_write");
+}
+
+kq_status kq_kv_cache_read(const kq_kv_cache* cache, const int64_t* slots, int64_t T, void* k, void* v, kq_dtype dtype, void* stream) {
+    if (T < 0 || T > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "T = %lld must be in [0, 2^31 - 1]", (long long)T);
+    if (!dtype_ok(dtype)) return fail(KQ_ERROR_INVALID_VALUE, "dtype = %d must be a kq_dtype", (int)dtype);
+    kq::CacheCopyParams p{};
+    const kq_status st = check_cache(cache, T > 0, &p.c);
+    if (st != KQ_SUCCESS || T == 0) return st;
+    if (!k || !v || !slots) return fail(KQ_ERROR_NULL_POINTER, "k, v and slots must not be NULL");
+    if (!aligned(k, 16) || !aligned(v, 16)) return fail(KQ_ERROR_MISALIGNED, "k and v must be 16-byte aligned");
+    if (!aligned(slots, 8)) return fail(KQ_ERROR_MISALIGNED, "slots must be 8-byte aligned");
+    p.slots = slots;
+    p.T = T;
+    p.k = k;
+    p.v = v;
+    p.is16 = dtype == KQ_DTYPE_BF16;
+    return from_hip(kq::launch_cache_read(p, (hipStream_t)stream), "kq_kv_cache_read");
+}
+
+static kq_status check_attention(int64_t B, int64_t q_heads, int64_t heads) {
+    if (B < 0 || B > (int64_t(1) << 20)) return fail(KQ_ERROR_INVALID_VALUE, "B = %lld must be in [0, 2^20]", (long long)B);
+    if (q_heads < 1 || q_heads > 65535 || q_heads % heads)
+        return fail(KQ_ERROR_INVALID_VALUE, "q_heads = %lld must be a multiple of the cache's %lld heads, at most 65535", (long long)q_heads,
+                    (long long)heads);
+    return ok();
+}
+
+kq_status kq_paged_attention_workspace_size(int64_t B, int64_t q_heads, int64_t heads, int64_t d, size_t* bytes) {
+    if (heads < 1 || heads > 65535) return fail(KQ_ERROR_INVALID_VALUE, "heads = %lld must be in [1, 65535]", (long long)heads);
+    if (d < 32 || d % 32 || d > kq::kCacheMaxColumns)
+        return fail(KQ_ERROR_INVALID_VALUE, "d = %lld must be a multiple of 32 in [32, %lld]", (long long)d, (long long)kq::kCacheMaxColumns);
+    const kq_status st = check_attention(B, q_heads, heads);
+    if (st != KQ_SUCCESS) return st;
+    if (!bytes) return fail(KQ_ERROR_NULL_POINTER, "bytes must not be NULL");
+    *bytes = (size_t)std::max<int64_t>(16, kq::attn_workspace(B, heads, q_heads / heads, d));
+    return ok();
+}
+
+kq_status kq_paged_attention(const void* q, kq_dtype dtype, int64_t B, int64_t q_heads, int64_t q_seq, int64_t q_head,
+                             const kq_kv_cache* cache, const int32_t* page_table, int64_t table_stride, int64_t max_pages,
+                             const int32_t* lengths, float scale, int64_t window, void* out, int64_t out_seq, int64_t out_head,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    kq::AttnParams p{};
+    kq_status st = check_cache(cache, B > 0, &p.c);
+    if (st == KQ_SUCCESS) st = check_attention(B, q_heads, cache->heads);
+    if (st != KQ_SUCCESS) return st;
+    if (!dtype_ok(dtype)) return fail(KQ_ERROR_INVALID_VALUE, "dtype = %d must be a kq_dtype", (int)dtype);
+    if (q_seq < 0 || q_head < 0 || out_seq < 0 || out_head < 0 || table_stride < 0)
+        return fail(KQ_ERROR_INVALID_VALUE, "strides must be >= 0");
+    if (max_pages < 0 || max_pages > INT32_MAX) return fail(KQ_ERROR_INVALID_VALUE, "max_pages = %lld must be in [0, 2^31 - 1]", (long long)max_pages);
+    if (window < 0) return fail(KQ_ERROR_INVALID_VALUE, "window = %lld must be >= 0", (long long)window);
+    if (!std::isfinite(scale)) return fail(KQ_ERROR_INVALID_VALUE, "scale must be finite");
+    if ((B > 1 && out_seq < cache->d) || (q_heads > 1 && out_head < cache->d)) return fail(KQ_ERROR_INVALID_VALUE, "the rows of out overlap");
+    if (B == 0) return ok();
+    if (!q || !out || !lengths || !workspace || (!page_table && max_pages > 0))
+        return fail(KQ_ERROR_NULL_POINTER, "q, page_table, lengths, out and workspace must not be NULL");
+    if (!aligned(q, dtype_bytes(dtype)) || !aligned(out, dtype_bytes(dtype)) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(lse, 4))
+        return fail(KQ_ERROR_MISALIGNED, "q, page_table, lengths, out and lse must be aligned to their elements");
+    if (!aligned(workspace, 16)) return fail(KQ_ERROR_MISALIGNED, "workspace must be 16-byte aligned");
+    const int64_t group = q_heads / cache->heads, need = kq::attn_workspace(B, cache->heads, group, cache->d);
+    if (workspace_bytes < (size_t)need)
+        return fail(KQ_ERROR_INVALID_VALUE, "workspace holds %zu bytes, the call needs %lld", workspace_bytes, (long long)need);
+    p.q = q;
+    p.out = out;
+    p.q_seq = q_seq;
+    p.q_head = q_head;
+    p.out_seq = out_seq;
+    p.out_head = out_head;
+    p.B = B;
+    p.group = (int)group;
+    p.table = page_table;
+    p.table_stride = table_stride;
+    p.max_tokens = std::min<int64_t>(max_pages * cache->page_size, int64_t(INT32_MAX) - 63);
+    p.lengths = lengths;
+    p.window = window;
+    p.scale = scale;
+    p.is16 = dtype == KQ_DTYPE_BF16;
+    p.lse = lse;
+    p.workspace = static_cast<uint8_t*>(workspace);
+    return from_hip(kq::launch_attn(p, (hipStream_t)stream), "kq_paged_attention");
+}
+
+kq_status kq_w4a16_linear(const void* x, kq_dtype x_dtype, int64_t M, int64_t ldx, const uint8_t* b_codes,
+                          const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
+                          int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act, const void* residual,
+                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream) {
+    if (!dtype_ok(x_dtype)) return fail(KQ_ERROR_INVALID_VALUE, "x_dtype = %d must be a kq_dtype", (int)x_dtype);
+    // (the weight stands in for the operand that this call does not have)
+    const kq_status st = check_linear(b_codes, b_scales, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    if (st != KQ_SUCCESS) return st;
+    const int64_t cols = act == KQ_ACT_SWIGLU ? N / 2 : N;
+    if (M > 65535 * 16) return fail(KQ_ERROR_INVALID_VALUE, "M = %lld is too large (at most 65535 * 16)", (long long)M);
+    if (ldx < K) return fail(KQ_ERROR_INVALID_VALUE, "ldx = %lld must be >= %lld", (long long)ldx, (long long)K);
+    if (gate && (gate_rows < 1 || gate_stride < 0))
+        return fail(KQ_ERROR_INVALID_VALUE, "gate_rows = %lld must be >= 1 and gate_stride = %lld >= 0", (long long)gate_rows, (long long)gate_stride);
+    if (residual && ldr < cols) return fail(KQ_ERROR_INVALID_VALUE, "ldr = %lld must be >= %lld", (long long)ldr, (long long)cols);
+    if (!aligned(gate, dtype_bytes(vec_dtype)) || !aligned(residual, dtype_bytes(out_dtype)))
+        return fail(KQ_ERROR_MISALIGNED, "gate and residual must be aligned to their elements");
+    if (M == 0 || N == 0) return ok();
+    if (!x) return fail(KQ_ERROR_NULL_POINTER, "x must not be NULL");
+    if (!aligned(x, dtype_bytes(x_dtype))) return fail(KQ_ERROR_MISALIGNED, "x must be aligned to its elements");
+    kq::MatvecParams p{};
+    p.x = x;
+    p.ldx = ldx;
+    p.x16 = x_dtype == KQ_DTYPE_BF16;
+    p.l = linear_params(nullptr, nullptr, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
+    p.l.gate = gate;
+    p.l.gate_stride = gate_stride;
+    p.l.gate_rows = gate ? gate_rows : 1;
+    p.l.residual = residual;
+    p.l.ldr = ldr;
+    return from_hip(kq::launch_matvec(p, (hipStream_t)stream), "kq_w4a16_linear");
 }
 
 kq_status kq_mxfp4_quantize(const uint16_t* X, int64_t M, int64_t d, uint8_t* codes, uint8_t* scales,

@@ -1,0 +1,469 @@
+// Attention of one new token of every sequence over a paged cache:
+//     out = softmax(scale q K^T) V
+// over the sequence's tokens (or its last `window`), K and V in bf16, MXFP8 or
+// MXFP4.  One pass over the cache with the running maximum and sum of the
+// softmax; ragged sequences are cut into parts of equal length (kq_split.h) and
+// joined by a second launch.
+//
+// A wave takes a tile of 32 tokens of one head of the cache and up to 16 of the
+// query heads that share it.  Both products run on the bf16 matrix cores, which
+// hold the cache's values of every format exactly:
+//     S^T = K Q^T   A: 16 tokens x 32 columns, lane (r, g) = row r, eight columns
+//     O^T = V^T P^T A: 16 columns x 32 tokens, lane (r, g) = column r, tokens 8 g .. 8 g + 7
+// (r = lane % 16, g = lane / 16).  Row r of S^T's tile m is token
+// 8 (r / 4) + 4 m + r % 4, so that a lane's eight results, rows 4 g .. 4 g + 3 of
+// two tiles, are query r's scores of tokens 8 g .. 8 g + 7: P^T's operand as it
+// is, without an exchange between lanes.  The order of the columns in S^T's sum
+// is free, so each lane's columns of K are 16 bytes side by side; V's columns
+// that a lane loads of its eight tokens are turned into operands by byte
+// permutations.  Operands of 32 bits (q, and the softmax's p in any case) go in
+// as two or three bf16 terms: p = hi + lo within 2^-17 p for a bf16 result, q
+// and p as three terms, exact to 2^-24, for a 32-bit one.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "kq_mx.h"
+#include "kq_serve.h"
+#include "kq_split.h"
+
+namespace kq {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kAttnWaves = 4;
+constexpr int kAttnThreads = 64 * kAttnWaves;
+constexpr int kAttnGroups = 1024;  // workgroups that a call's parts are cut for
+constexpr int kRowTile = 16;       // query heads of a workgroup
+
+template <CacheFormat F>
+constexpr int kBits = F == CacheFormat::Bf16 ? 16 : F == CacheFormat::Mxfp8 ? 8 : 4;
+
+constexpr int least(int a, int b) { return a < b ? a : b; }
+
+// N bytes (2, 4, 8 or 16) at p.
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[(N + 3) / 4]) {
+    if constexpr (N == 2) {
+        w[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else if constexpr (N == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N == 8) {
+        const u32x2v v = *reinterpret_cast<const u32x2v*>(p);
+        w[0] = v[0];
+        w[1] = v[1];
+    } else {
+        const u32x4v v = *reinterpret_cast<const u32x4v*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = v[k];
+    }
+}
+
+// Values 2 I and 2 I + 1 of a row's loaded words, as bf16.
+template <CacheFormat F, int I, int W>
+__device__ __forceinline__ uint32_t pair_of(const uint32_t (&w)[W], float scale) {
+    if constexpr (F == CacheFormat::Bf16) return w[I];
+    else if constexpr (F == CacheFormat::Mxfp8) return e4m3_pair<I % 2>(w[I / 2], scale);
+    else return e2m1_pair<I % 4>(w[I / 4], scale);
+}
+
+__device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_bit_cast(bf16x8, u32x4v{a, b, c, d});
+}
+
+// Eight values in 32 bits as TERMS bf16 operands whose sum they are: the leading bits as they stand, what is left
+// rounded in the last.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float (&v)[8], bf16x8 (&t)[TERMS]) {
+    float f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = v[k];
+#pragma unroll
+    for (int n = 0; n < TERMS; ++n) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (n + 1 == TERMS) {
+                w[k] = bf16_pair(f[2 * k], f[2 * k + 1]);
+            } else {
+                w[k] = __builtin_amdgcn_perm(__float_as_uint(f[2 * k + 1]), __float_as_uint(f[2 * k]), 0x07060302u);
+                f[2 * k] -= bf16_low(w[k]);
+                f[2 * k + 1] -= bf16_high(w[k]);
+            }
+        }
+        t[n] = operand(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// The same over the four lanes of a query (r, r + 16, r + 32, r + 48).
+__device__ __forceinline__ float query_max(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float query_sum(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+constexpr float kLowest = -3.402823466e38f;
+
+// DC: columns of the matrix products, at least d.
+template <CacheFormat F, int DC>
+struct Tile {
+    static constexpr int kE8 = kBits<F>;  // bytes of eight values
+    // K: a lane's columns of unit u are kKw from 4 kKw u + kKw g on
+    static constexpr int kSteps = DC / 32, kKs = least(kSteps, 16 / kE8), kKw = 8 * kKs, kKu = kSteps / kKs;
+    static constexpr int kKb = kKs * kE8, kKwords = (kKb + 3) / 4;
+    // V: a lane's columns of unit u are kVw from 16 kVw u + kVw r on
+    static constexpr int kVc = DC / 16, kVw = least(kVc, F == CacheFormat::Bf16 ? 8 : 16), kVu = kVc / kVw;
+    static constexpr int kVb = kVw * kE8 / 8, kVwords = (kVb + 3) / 4;
+    static constexpr bool kScaled = F != CacheFormat::Bf16;
+
+    uint32_t k[2][kKu][kKwords];
+    uint32_t v[8][kVu][kVwords];
+    uint32_t ks[2][kScaled ? kKu : 1];
+    uint32_t vs[8][kScaled ? kVu : 1];
+
+    // Tokens 32 t .. 32 t + 31 of head h, of which those before `end` exist: the page of a token past it is the last one's.
+    __device__ __forceinline__ void load(const Cache& c, const int32_t* table, int h, int t, int end) {
+        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+        const int base = t * kTileTokens;
+        int64_t page[2];  // of tokens 0 .. 15 and 16 .. 31
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t id = page_of(table[page_index(base + 16 * i, end, c.page_shift)], c.pages);
+            page[i] = ((id * c.heads + h) << c.page_shift) + ((base + 16 * i) & (c.page_size - 1));
+        }
+        const int dk = c.d * kE8 / 8, ds = c.d / 32;  // bytes of a row, and of its scales
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int64_t row = (r < 8 ? page[0] : page[1]) + (8 * (r >> 2) + 4 * m + (r & 3)) % 16;
+#pragma unroll
+            for (int u = 0; u < kKu; ++u) {
+                const int column = 4 * kKw * u + kKw * g;
+#pragma unroll
+                for (int i = 0; i < kKwords; ++i) k[m][u][i] = 0u;
+                if (kScaled) ks[m][u] = 127u;
+                if (column < c.d) {
+                    load_words<kKb>(c.k + row * dk + column * kE8 / 8, k[m][u]);
+                    if (kScaled) ks[m][u] = c.k_scales[row * ds + column / 32];
+                }
+            }
+        }
+        const int64_t first = (g < 2 ? page[0] : page[1]) + 8 * (g & 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int u = 0; u < kVu; ++u) {
+                const int column = 16 * kVw * u + kVw * r;
+#pragma unroll
+                for (int i = 0; i < kVwords; ++i) v[j][u][i] = 0u;
+                if (kScaled) vs[j][u] = 127u;
+                if (column < c.d) {
+                    load_words<kVb>(c.v + (first + j) * dk + column * kE8 / 8, v[j][u]);
+                    if (kScaled) vs[j][u] = c.v_scales[(first + j) * ds + column / 32];
+                }
+            }
+        }
+    }
+
+    // Values of tokens that do not count are zero, whatever the cache holds there.
+    __device__ __forceinline__ void clear(int t, int from, int end) {
+        const int token = t * kTileTokens + 8 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (token + j >= from && token + j < end) continue;
+#pragma unroll
+            for (int u = 0; u < kVu; ++u) {
+#pragma unroll
+                for (int i = 0; i < kVwords; ++i) v[j][u][i] = 0u;
+                if (kScaled) vs[j][u] = 127u;
+            }
+        }
+    }
+
+    // Unit u's columns of step w of K's tile m.
+    template <int W>
+    __device__ __forceinline__ bf16x8 keys(int m, int u) const {
+        const float s = kScaled ? mx_scale(ks[m][kScaled ? u : 0]) : 0.f;
+        return operand(pair_of<F, 4 * W>(k[m][u], s), pair_of<F, 4 * W + 1>(k[m][u], s), pair_of<F, 4 * W + 2>(k[m][u], s),
+                       pair_of<F, 4 * W + 3>(k[m][u], s));
+    }
+    // Columns 2 I and 2 I + 1 of V's unit u, eight tokens each.
+    template <int I>
+    __device__ __forceinline__ void values(int u, bf16x8 (&a)[2]) const {
+        uint32_t x[8], lo[4], hi[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = pair_of<F, I>(v[j][u], kScaled ? mx_scale(vs[j][kScaled ? u : 0]) : 0.f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
+            hi[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
+        }
+        a[0] = operand(lo[0], lo[1], lo[2], lo[3]);
+        a[1] = operand(hi[0], hi[1], hi[2], hi[3]);
+    }
+};
+
+template <int I, int N, class Fn>
+__device__ __forceinline__ void unrolled(Fn f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<I + 1, N>(f);
+    }
+}
+
+// The column of O^T's tile n, row i.
+template <CacheFormat F, int DC>
+__device__ __forceinline__ int value_column(int n, int i) {
+    constexpr int w = Tile<F, DC>::kVw;
+    return 16 * w * (n / w) + w * i + n % w;
+}
+
+template <CacheFormat F, int DC, bool B16>
+__global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnParams p) {
+    typedef Tile<F, DC> T;
+    constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
+    const Cache& c = p.c;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const Part part = find_part(p.lengths, (int)p.B, p.max_tokens, p.window, p.parts, (int)blockIdx.x);
+    if (part.b < 0) return;
+    const int row_tiles = (p.group + kRowTile - 1) / kRowTile;
+    const int h = blockIdx.y / row_tiles, first_row = (blockIdx.y - h * row_tiles) * kRowTile;
+    const int rows = min(p.group - first_row, kRowTile), head = h * p.group + first_row;
+    if (part.index == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        p.plan[2 * part.b] = part.slot;
+        p.plan[2 * part.b + 1] = part.count;
+    }
+    const int32_t* const table = p.table + part.b * p.table_stride;
+
+    bf16x8 q[T::kSteps][kQ];
+    unrolled<0, T::kSteps>([&](auto step) {
+        constexpr int u = step / T::kKs, w = step % T::kKs;
+        const int column = 4 * T::kKw * u + T::kKw * g + 8 * w;
+        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r < rows && column < c.d) {
+            const int64_t at = part.b * p.q_seq + (head + r) * p.q_head + column;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                f[k] = B16 ? bf16_low(static_cast<const uint16_t*>(p.q)[at + k]) : static_cast<const float*>(p.q)[at + k];
+        }
+        split_terms<kQ>(f, q[step]);
+    });
+
+    f32x4 o[T::kVc];
+#pragma unroll
+    for (int n = 0; n < T::kVc; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float most = kLowest, sum = 0.f;
+    const float scale = p.scale * 1.44269504088896341f;  // scores in powers of two
+    for (int i = wave; i < part.tiles; i += kAttnWaves) {
+        const int t = part.tile + i;
+        T tile;
+        tile.load(c, table, h, t, part.end);
+        const bool edge = t * kTileTokens < part.first || (t + 1) * kTileTokens > part.end;
+        if (edge) tile.clear(t, part.first, part.end);
+        float s[8];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            f32x4 a = {0.f, 0.f, 0.f, 0.f};
+            unrolled<0, T::kSteps>([&](auto step) {
+                constexpr int u = step / T::kKs, w = step % T::kKs;
+                const bf16x8 k = tile.template keys<w>(m, u);
+#pragma unroll
+                for (int n = 0; n < kQ; ++n) a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[step][n], a, 0, 0, 0);
+            });
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[4 * m + k] = a[k] * scale;
+        }
+        if (edge) {
+            const int token = t * kTileTokens + 8 * g;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (token + k < part.first || token + k >= part.end) s[k] = -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) top = fmaxf(top, s[k]);
+        top = fmaxf(query_max(top), most);
+        if (__any(top > most)) {
+            const float f = __builtin_amdgcn_exp2f(most - top);
+            sum *= f;
+#pragma unroll
+            for (int n = 0; n < T::kVc; ++n) o[n] *= f;
+            most = top;
+        }
+        float e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            e[k] = __builtin_amdgcn_exp2f(s[k] - most);
+            sum += e[k];
+        }
+        bf16x8 pt[kP];
+        split_terms<kP>(e, pt);
+#pragma unroll
+        for (int u = 0; u < T::kVu; ++u) {
+            unrolled<0, T::kVw / 2>([&](auto pair) {
+                bf16x8 a[2];
+                tile.template values<pair>(u, a);
+#pragma unroll
+                for (int n = 0; n < kP; ++n) {
+                    f32x4 &x = o[u * T::kVw + 2 * pair], &y = o[u * T::kVw + 2 * pair + 1];
+                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], pt[n], x, 0, 0, 0);
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], pt[n], y, 0, 0, 0);
+                }
+            });
+        }
+    }
+
+    // The waves' results in one: the common maximum first, then sums.
+    extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3
+    __shared__ float stats[2][kAttnWaves][kRowTile];
+    sum = query_sum(sum);
+    if (g == 0) {
+        stats[0][wave][r] = most;
+        stats[1][wave][r] = sum;
+    }
+    __syncthreads();
+    float all = stats[0][0][r];
+#pragma unroll
+    for (int w = 1; w < kAttnWaves; ++w) all = fmaxf(all, stats[0][w][r]);
+    const float f = __builtin_amdgcn_exp2f(most - all);
+    static_assert(kAttnWaves == 4, "two waves a place");
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+        if (wave / 2 == turn && r < rows) {
+#pragma unroll
+            for (int n = 0; n < T::kVc; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int column = value_column<F, DC>(n, 4 * g + k);
+                    if (column >= c.d) continue;
+                    float& v = shared[((wave & 1) * rows + r) * c.d + column];
+                    v = turn ? v + o[n][k] * f : o[n][k] * f;
+                }
+        }
+        __syncthreads();
+    }
+    const bool whole = part.count == 1;
+    const int64_t place = (part.slot + part.index) * (int64_t)(c.heads * p.group) + head;  // of a part's results
+    for (int i = threadIdx.x; i < rows * c.d; i += kAttnThreads) {
+        const int row = i / c.d, column = i - row * c.d;
+        float top = stats[0][0][row], total = 0.f;
+        float v = shared[row * c.d + column] + shared[(rows + row) * c.d + column];
+#pragma unroll
+        for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stats[0][w][row]);
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) total += stats[1][w][row] * __builtin_amdgcn_exp2f(stats[0][w][row] - top);
+        if (whole) {
+            v = total != 0.f ? v / total : 0.f;
+            const int64_t at = part.b * p.out_seq + (head + row) * p.out_head + column;
+            if (B16) static_cast<__bf16*>(p.out)[at] = (__bf16)v;
+            else static_cast<float*>(p.out)[at] = v;
+            if (p.lse && column == 0)
+                p.lse[part.b * (int64_t)(c.heads * p.group) + head + row] =
+                    total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945309f : -INFINITY;
+        } else {
+            p.partial[(place + row) * c.d + column] = v;
+            if (column == 0) {
+                p.stats[2 * (place + row)] = top;
+                p.stats[2 * (place + row) + 1] = total;
+            }
+        }
+    }
+}
+
+// Parts' results in one, a workgroup a sequence and query head.
+template <bool B16>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+    const int b = blockIdx.x, head = blockIdx.y, d = p.c.d, heads = p.c.heads * p.group;
+    const int slot = p.plan[2 * b], count = p.plan[2 * b + 1];
+    if (count <= 1) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)slot * heads + head;
+    float top = kLowest;
+    for (int i = lane; i < count; i += 64) top = fmaxf(top, p.stats[2 * (first + (int64_t)i * heads)]);
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};  // columns lane, lane + 64, ...
+    for (int i = wave; i < count; i += 4) {
+        const int64_t at = first + (int64_t)i * heads;
+        const float f = __builtin_amdgcn_exp2f(p.stats[2 * at] - top);
+        total += f * p.stats[2 * at + 1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (lane + 64 * k < d) v[k] += f * p.partial[at * d + lane + 64 * k];
+    }
+    __shared__ float sums[4], part[4][256];
+    if (lane == 0) sums[wave] = total;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = v[k];
+    __syncthreads();
+    total = sums[0] + sums[1] + sums[2] + sums[3];
+    if ((int)threadIdx.x < d) {
+        const int i = threadIdx.x;
+        const float f = total != 0.f ? (part[0][i] + part[1][i] + part[2][i] + part[3][i]) / total : 0.f;
+        const int64_t at = b * p.out_seq + head * p.out_head + i;
+        if (B16) static_cast<__bf16*>(p.out)[at] = (__bf16)f;
+        else static_cast<float*>(p.out)[at] = f;
+    }
+    if (p.lse && threadIdx.x == 0)
+        p.lse[(int64_t)b * heads + head] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945309f : -INFINITY;
+}
+
+int attn_parts(int64_t heads, int64_t group) {
+    return (int)std::max<int64_t>(1, kAttnGroups / (heads * ((group + kRowTile - 1) / kRowTile)));
+}
+
+int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
+
+template <CacheFormat F, int DC>
+void launch_attn_of(const AttnParams& p, dim3 grid, size_t lds, hipStream_t st) {
+    if (p.is16) attn_kernel<F, DC, true><<<grid, kAttnThreads, lds, st>>>(p);
+    else attn_kernel<F, DC, false><<<grid, kAttnThreads, lds, st>>>(p);
+}
+
+template <CacheFormat F>
+void launch_attn_format(const AttnParams& p, dim3 grid, size_t lds, hipStream_t st) {
+    if (p.c.d <= 64) launch_attn_of<F, 64>(p, grid, lds, st);
+    else if (p.c.d <= 128) launch_attn_of<F, 128>(p, grid, lds, st);
+    else launch_attn_of<F, 256>(p, grid, lds, st);
+}
+
+}  // namespace
+
+int64_t attn_workspace(int64_t B, int64_t heads, int64_t group, int64_t d) {
+    const int64_t rows = part_slots(attn_parts(heads, group), B) * heads * group;
+    return round16(8 * B) + round16(8 * rows) + round16(4 * rows * d);
+}
+
+hipError_t launch_attn(AttnParams p, hipStream_t st) {
+    const int heads = p.c.heads * p.group, row_tiles = (p.group + kRowTile - 1) / kRowTile;
+    p.parts = attn_parts(p.c.heads, p.group);
+    p.slots = part_slots(p.parts, p.B);
+    p.plan = reinterpret_cast<int32_t*>(p.workspace);
+    p.stats = reinterpret_cast<float*>(p.workspace + round16(8 * p.B));
+    p.partial = reinterpret_cast<float*>(p.workspace + round16(8 * p.B) + round16(8 * p.slots * heads));
+    const dim3 grid((unsigned)(p.parts + p.B), (unsigned)(p.c.heads * row_tiles));
+    const size_t lds = sizeof(float) * 2 * std::min(p.group, kRowTile) * p.c.d;
+    switch (p.c.format) {
+        case CacheFormat::Bf16: launch_attn_format<CacheFormat::Bf16>(p, grid, lds, st); break;
+        case CacheFormat::Mxfp8: launch_attn_format<CacheFormat::Mxfp8>(p, grid, lds, st); break;
+        case CacheFormat::Mxfp4: launch_attn_format<CacheFormat::Mxfp4>(p, grid, lds, st); break;
+    }
+    const hipError_t e = hipGetLastError();
+    // a table of no more tokens than the least part has holds no sequence of several parts
+    if (e != hipSuccess || p.max_tokens <= kLeastTiles * kTileTokens) return e;
+    const dim3 joins((unsigned)p.B, (unsigned)heads);
+    if (p.is16) attn_join_kernel<true><<<joins, 256, 0, st>>>(p);
+    else attn_join_kernel<false><<<joins, 256, 0, st>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace kq

@@ -9,12 +9,14 @@
 // checks and ctypes for a kernel of 2.8.
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "kroquant.h"
 
@@ -625,12 +627,338 @@ PyObject* block_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------ a generation step
+
+// The device is current: a launch, and the current stream, are on it.
+bool current(at::Device dev) { return dev.is_cuda() && dev.index() == c10::hip::current_device(); }
+
+// A [rows, heads, columns] array of fp32 or bf16 whose columns are contiguous.
+struct Heads {
+    const at::Tensor* t = nullptr;
+    int type = 0;
+    int64_t T = 0, H = 0, D = 0, row = 0, head = 0;
+    bool parse(const at::Tensor* x) {
+        t = x;
+        if (!t || !t->is_cuda() || t->dim() != 3 || !float_type(t, &type)) return false;
+        T = t->size(0);
+        H = t->size(1);
+        D = t->size(2);
+        if (D > 1 && t->stride(2) != 1) return false;
+        row = T > 1 ? t->stride(0) : H * D;
+        head = H > 1 ? t->stride(1) : D;
+        return true;
+    }
+};
+
+// A result of x's sizes and type: a new one, x itself, or a contiguous one that shares no memory with x (others are
+// left to Python's checks).
+struct HeadsOut {
+    Out out;
+    int64_t row, head;
+    bool parse(PyObject* o, const Heads& x) {
+        row = x.H * x.D;
+        head = x.D;
+        if (o == Py_None) {
+            out.made = empty({x.T, x.H, x.D}, x.t->scalar_type(), x.t->device());
+            out.ptr = out.made.data_ptr();
+            return true;
+        }
+        const at::Tensor* t = tensor(o);
+        if (!t || t->scalar_type() != x.t->scalar_type() || t->device() != x.t->device() || !t->sizes().equals(x.t->sizes()) ||
+            !t->is_contiguous())
+            return false;
+        const bool same = t->data_ptr() == x.t->data_ptr() && t->strides().equals(x.t->strides());
+        if (!same && t->storage().data() == x.t->storage().data()) return false;
+        out.given = o;
+        out.ptr = t->data_ptr();
+        return true;
+    }
+};
+
+// (x, positions, axes, theta, pairing, freqs, backward, out, stream)
+PyObject* rope(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 9) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        Heads x;
+        HeadsOut y;
+        int pairing;
+        bool backward;
+        void* st = nullptr;
+        double theta;
+        if (!x.parse(tensor(v[0])) || !current(x.t->device()) || !small_int(v[4], &pairing) || !flag(v[6], &backward) ||
+            !stream_of(v[8], &st))
+            return nullptr;
+        if (PyFloat_CheckExact(v[3])) theta = PyFloat_AS_DOUBLE(v[3]);
+        else return nullptr;
+        const at::Tensor* pos = tensor(v[1]);
+        if (!pos || pos->device() != x.t->device()) return nullptr;
+        int type;
+        if (pos->scalar_type() == at::kInt) type = KQ_POSITION_INT32;
+        else if (pos->scalar_type() == at::kLong) type = KQ_POSITION_INT64;
+        else if (pos->scalar_type() == at::kFloat) type = KQ_POSITION_FP32;
+        else return nullptr;
+        int axes[4], count = 0;
+        int64_t pairs = 0;
+        if (PyLong_CheckExact(v[2])) {
+            axes[count++] = (int)PyLong_AsLong(v[2]);
+        } else {
+            const bool list = PyList_CheckExact(v[2]);
+            if (!list && !PyTuple_CheckExact(v[2])) return nullptr;
+            const Py_ssize_t m = list ? PyList_GET_SIZE(v[2]) : PyTuple_GET_SIZE(v[2]);
+            if (m < 1 || m > 4) return nullptr;
+            while (count < m) {
+                PyObject* const o = list ? PyList_GET_ITEM(v[2], count) : PyTuple_GET_ITEM(v[2], count);
+                if (!small_int(o, &axes[count])) return nullptr;
+                ++count;
+            }
+        }
+        if (PyErr_Occurred()) return nullptr;
+        for (int i = 0; i < count; ++i) pairs += axes[i] / 2;
+        const bool flat = pos->dim() == 1 && count == 1;
+        if (!flat && (pos->dim() != 2 || pos->size(1) != count || (count > 1 && pos->stride(1) != 1))) return nullptr;
+        if (pos->size(0) != x.T) return nullptr;
+        const at::Tensor* freqs = nullptr;
+        if (v[5] != Py_None) {
+            freqs = tensor(v[5]);
+            if (!buffer(freqs, at::kDouble, pairs, x.t->device())) return nullptr;
+        }
+        if (!y.parse(v[7], x)) return nullptr;
+        if (!call("kq_rope", [&] {
+                return kq_rope(x.t->data_ptr(), (kq_dtype)x.type, x.T, x.H, x.D, x.row, x.head, pos->data_ptr(), (kq_position)type,
+                               x.T > 1 ? pos->stride(0) : count, axes, count, theta,
+                               freqs ? static_cast<const double*>(freqs->data_ptr()) : nullptr, (kq_pairing)pairing, backward,
+                               y.out.ptr, y.row, y.head, st);
+            }))
+            return nullptr;
+        return y.out.take();
+    });
+}
+
+// A KVCache (a named tuple of four).
+bool cache_of(PyObject* o, kq_kv_cache* c, at::Device* dev) {
+    if (!PyTuple_Check(o) || PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) return false;
+    static PyObject* type = nullptr;  // (the GIL is held)
+    if (!type) {
+        PyObject* const m = PyImport_ImportModule("paper_2607_21446_amd.binding");
+        type = m ? PyObject_GetAttrString(m, "KVCache") : nullptr;
+        Py_XDECREF(m);
+        if (!type) return false;
+    }
+    if (reinterpret_cast<PyObject*>(Py_TYPE(o)) != type) return false;
+    const bool scaled = PyTuple_GET_ITEM(o, 2) != Py_None;
+    if (scaled != (PyTuple_GET_ITEM(o, 3) != Py_None)) return false;
+    const at::Tensor* t[4] = {nullptr, nullptr, nullptr, nullptr};
+    for (int i = 0; i < (scaled ? 4 : 2); ++i) {
+        t[i] = tensor(PyTuple_GET_ITEM(o, i));
+        if (!dense(t[i], scaled ? at::kByte : at::kBFloat16) || t[i]->dim() != 4 || t[i]->device() != t[0]->device()) return false;
+        if (i % 2 && !t[i]->sizes().equals(t[i - 1]->sizes())) return false;
+    }
+    const int64_t row = t[0]->size(3);
+    c->d = row;
+    c->format = KQ_CACHE_BF16;
+    if (scaled) {
+        for (int i = 0; i < 3; ++i)
+            if (t[2]->size(i) != t[0]->size(i)) return false;
+        c->d = 32 * t[2]->size(3);
+        if (row != c->d && 2 * row != c->d) return false;
+        c->format = row == c->d ? KQ_CACHE_MXFP8 : KQ_CACHE_MXFP4;
+    }
+    c->k = t[0]->data_ptr();
+    c->v = t[1]->data_ptr();
+    c->k_scales = scaled ? static_cast<uint8_t*>(t[2]->data_ptr()) : nullptr;
+    c->v_scales = scaled ? static_cast<uint8_t*>(t[3]->data_ptr()) : nullptr;
+    c->pages = t[0]->size(0);
+    c->heads = t[0]->size(1);
+    c->page_size = t[0]->size(2);
+    *dev = t[0]->device();
+    return current(*dev);
+}
+
+const at::Tensor* slots_of(PyObject* o, at::Device dev) {
+    const at::Tensor* t = tensor(o);
+    return dense(t, at::kLong) && t->dim() == 1 && t->device() == dev ? t : nullptr;
+}
+
+// (cache, k, v, slots, stream)
+PyObject* kv_cache_write(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 5) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        kq_kv_cache c;
+        at::Device dev = at::kCPU;
+        Heads h[2];
+        void* st = nullptr;
+        if (!cache_of(v[0], &c, &dev) || !stream_of(v[4], &st)) return nullptr;
+        const at::Tensor* slots = slots_of(v[3], dev);
+        if (!slots) return nullptr;
+        for (int i = 0; i < 2; ++i) {
+            if (!h[i].parse(tensor(v[1 + i])) || h[i].t->device() != dev || h[i].type != h[0].type || h[i].T != slots->numel() ||
+                h[i].H != c.heads || h[i].D != c.d)
+                return nullptr;
+        }
+        if (!call("kq_kv_cache_write", [&] {
+                return kq_kv_cache_write(&c, h[0].t->data_ptr(), h[1].t->data_ptr(), (kq_dtype)h[0].type, h[0].T, h[0].row, h[0].head,
+                                         h[1].row, h[1].head, static_cast<const int64_t*>(slots->data_ptr()), st);
+            }))
+            return nullptr;
+        Py_INCREF(v[0]);
+        return v[0];
+    });
+}
+
+// (cache, slots, k, v, out_dtype, stream)
+PyObject* kv_cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 6) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        kq_kv_cache c;
+        at::Device dev = at::kCPU;
+        void* st = nullptr;
+        if (!cache_of(v[0], &c, &dev) || !stream_of(v[5], &st)) return nullptr;
+        const at::Tensor* slots = slots_of(v[1], dev);
+        if (!slots) return nullptr;
+        at::ScalarType type = at::kBFloat16;
+        if (v[4] != Py_None) {
+            if (!float_dtype(v[4], &type)) return nullptr;
+        } else if (v[2] != Py_None || v[3] != Py_None) {
+            const at::Tensor* t = tensor(v[2] != Py_None ? v[2] : v[3]);
+            if (!t) return nullptr;
+            type = t->scalar_type();
+        }
+        if (type != at::kFloat && type != at::kBFloat16) return nullptr;
+        const int64_t T = slots->numel();
+        Out out[2];
+        for (int i = 0; i < 2; ++i) {
+            if (v[2 + i] != Py_None) {
+                const at::Tensor* t = tensor(v[2 + i]);
+                if (!t || t->dim() != 3 || t->size(0) != T || t->size(1) != c.heads || t->size(2) != c.d) return nullptr;
+            }
+            if (!output(v[2 + i], true, {T, c.heads, c.d}, type, T * c.heads * c.d, dev, out[i])) return nullptr;
+        }
+        if (!call("kq_kv_cache_read", [&] {
+                return kq_kv_cache_read(&c, static_cast<const int64_t*>(slots->data_ptr()), T, out[0].ptr, out[1].ptr,
+                                        type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, st);
+            }))
+            return nullptr;
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, out[0].take());
+        PyTuple_SET_ITEM(r, 1, out[1].take());
+        return r;
+    });
+}
+
+// (q, cache, page_table, lengths, scale, window, out, lse, want_lse, workspace, stream)
+PyObject* paged_attention(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        kq_kv_cache c;
+        at::Device dev = at::kCPU;
+        Heads q;
+        HeadsOut out;
+        void* st = nullptr;
+        bool want = false;
+        if (!cache_of(v[1], &c, &dev) || !q.parse(tensor(v[0])) || q.t->device() != dev || q.D != c.d || q.H < 1 || c.heads < 1 ||
+            q.H % c.heads || !flag(v[8], &want) || !stream_of(v[10], &st))
+            return nullptr;
+        const at::Tensor *table = tensor(v[2]), *lengths = tensor(v[3]);
+        if (!table || !table->is_cuda() || table->scalar_type() != at::kInt || table->device() != dev || table->dim() != 2 ||
+            table->size(0) != q.T || (table->size(1) > 1 && table->stride(1) != 1) || !buffer(lengths, at::kInt, q.T, dev) ||
+            lengths->dim() != 1)
+            return nullptr;
+        float scale = (float)(1.0 / std::sqrt((double)c.d));
+        if (v[4] != Py_None && !number(v[4], &scale)) return nullptr;
+        int64_t window = 0;
+        if (v[5] != Py_None) {
+            if (!PyLong_CheckExact(v[5])) return nullptr;
+            window = PyLong_AsLongLong(v[5]);
+            if (window < 1) return nullptr;
+        }
+        if (!out.parse(v[6], q)) return nullptr;
+        Out lse;
+        if (v[7] != Py_None || want) {
+            if (!output(v[7], true, {q.T, q.H}, at::kFloat, q.T * q.H, dev, lse)) return nullptr;
+        }
+        size_t bytes = 0;
+        at::Tensor made;
+        void* work;
+        if (v[9] != Py_None) {
+            const at::Tensor* w = tensor(v[9]);
+            if (!dense(w, at::kByte) || w->device() != dev) return nullptr;
+            work = w->data_ptr();
+            bytes = w->numel();
+        } else {  // (one of the current stream's; for another stream Python makes it)
+            if (v[10] != Py_None || kq_paged_attention_workspace_size(q.T, q.H, c.heads, c.d, &bytes) != KQ_SUCCESS) return nullptr;
+            made = empty({(int64_t)bytes}, at::kByte, dev);
+            work = made.data_ptr();
+        }
+        if (!call("kq_paged_attention", [&] {
+                return kq_paged_attention(q.t->data_ptr(), (kq_dtype)q.type, q.T, q.H, q.row, q.head, &c,
+                                          static_cast<const int32_t*>(table->data_ptr()), q.T > 1 ? table->stride(0) : table->size(1),
+                                          table->size(1), static_cast<const int32_t*>(lengths->data_ptr()), scale, window, out.out.ptr,
+                                          out.row, out.head, static_cast<float*>(lse.ptr), work, bytes, st);
+            }))
+            return nullptr;
+        if (!lse.ptr && !lse.given && !lse.made.defined()) return out.out.take();
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, out.out.take());
+        PyTuple_SET_ITEM(r, 1, lse.take());
+        return r;
+    });
+}
+
+// (x, b_codes, b_scales, bias, act, gate, residual, out, out_dtype, stream)
+PyObject* w4a16_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != 10) Py_RETURN_NONE;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *x = tensor(v[0]), *b = tensor(v[1]), *s = tensor(v[2]);
+        int act, xt;
+        void* st = nullptr;
+        if (!x || !x->is_cuda() || x->dim() != 2 || !float_type(x, &xt) || !matrix(b, at::kByte) || !matrix(s, at::kByte) ||
+            !small_int(v[4], &act) || !stream_of(v[9], &st))
+            return nullptr;
+        const at::Device dev = x->device();
+        const int64_t M = x->size(0), K = x->size(1), N = b->size(0);
+        if (!current(dev) || b->device() != dev || s->device() != dev || 2 * b->size(1) != K || s->size(0) != N || s->size(1) != K / 32)
+            return nullptr;
+        const int64_t ldx = row_stride(x, M, K, x->scalar_type(), dev), cols = act == KQ_ACT_SWIGLU ? N / 2 : N;
+        if (ldx < 0 || (act == KQ_ACT_SWIGLU && N % 2)) return nullptr;
+        Vectors vec(dev);
+        const void *bias, *gate;
+        int64_t none, stride;
+        if (!vec.add(v[3], N, false, &bias, &none) || !vec.add(v[5], cols, true, &gate, &stride)) return nullptr;
+        if (vec.count() <= 0 || M % vec.count()) return nullptr;
+        at::ScalarType type = at::kBFloat16;
+        const at::Tensor* res = nullptr;
+        if (v[6] != Py_None) {
+            res = tensor(v[6]);
+            if (!res) return nullptr;
+            type = res->scalar_type();
+            if (type != at::kFloat && type != at::kBFloat16) return nullptr;
+        }
+        Out out;
+        int64_t ldo, ldr = 0;
+        if (!linear_out(v[7], v[8], type, M, cols, dev, out, &ldo, &type)) return nullptr;
+        if (res && (ldr = row_stride(res, M, cols, type, dev)) < 0) return nullptr;
+        if (!call("kq_w4a16_linear", [&] {
+                return kq_w4a16_linear(x->data_ptr(), (kq_dtype)xt, M, ldx, static_cast<const uint8_t*>(b->data_ptr()),
+                                       static_cast<const uint8_t*>(s->data_ptr()), N, K, bias, gate, stride,
+                                       std::max<int64_t>(1, M / vec.count()), (kq_dtype)vec.dtype(), (kq_act)act,
+                                       res ? res->data_ptr() : nullptr, ldr, out.ptr, ldo,
+                                       type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, st);
+            }))
+            return nullptr;
+        return out.take();
+    });
+}
+
 #define KQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {KQ_METHOD(quantize),    KQ_METHOD(quantize_exact), KQ_METHOD(quantize_packed),
                           KQ_METHOD(quantize_lu), KQ_METHOD(smoothquant),    KQ_METHOD(hadamard32),
                           KQ_METHOD(fwht),        KQ_METHOD(mxfp4),          KQ_METHOD(mxfp4_gemm),
                           KQ_METHOD(calib_step),  KQ_METHOD(mxfp4_linear),   KQ_METHOD(mxfp4_grouped_linear),
-                          KQ_METHOD(block_norm),  {nullptr, nullptr, 0, nullptr}};
+                          KQ_METHOD(block_norm),  KQ_METHOD(rope),           KQ_METHOD(kv_cache_write),
+                          KQ_METHOD(kv_cache_read), KQ_METHOD(paged_attention), KQ_METHOD(w4a16_linear),
+                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_kqbind", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
