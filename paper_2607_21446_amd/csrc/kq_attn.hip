@@ -115,8 +115,27 @@ __device__ __forceinline__ float query_sum(float v) {
 
 constexpr float kLowest = -3.402823466e38f;
 
-// DC: columns of the matrix products, at least d.
-template <CacheFormat F, int DC>
+// A uniform read of an array that the kernel does not write, by a scalar load.
+typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
+
+// Where a tile's tokens are: rows of a head in the cache for its tokens 0 .. 15 and 16 .. 31.
+struct Rows {
+    int64_t at[2];
+    // Tokens 32 t .. 32 t + 31 of head h, of which those before `end` exist.
+    __device__ __forceinline__ Rows(const Cache& c, const int32_t* table, int h, int t, int end) {
+        const int base = t * kTileTokens;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int token = base + 16 * i;
+            const int32_t entry = ((const_i32_ptr)table)[page_index(token, end, c.page_shift)];
+            at[i] = ((page_of(entry, c.pages) * c.heads + h) << c.page_shift) + (token & (c.page_size - 1));
+        }
+    }
+};
+
+// DC: columns of the matrix products, at least d; FULL: d itself.  Lanes of columns past d load the row's last ones:
+// q is 0 there, and those columns of the result are not stored.
+template <CacheFormat F, int DC, bool FULL>
 struct Tile {
     static constexpr int kE8 = kBits<F>;  // bytes of eight values
     // K: a lane's columns of unit u are kKw from 4 kKw u + kKw g on
@@ -132,46 +151,58 @@ struct Tile {
     uint32_t ks[2][kScaled ? kKu : 1];
     uint32_t vs[8][kScaled ? kVu : 1];
 
-    // Tokens 32 t .. 32 t + 31 of head h, of which those before `end` exist: the page of a token past it is the last one's.
-    __device__ __forceinline__ void load(const Cache& c, const int32_t* table, int h, int t, int end) {
-        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-        const int base = t * kTileTokens;
-        int64_t page[2];  // of tokens 0 .. 15 and 16 .. 31
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t id = page_of(table[page_index(base + 16 * i, end, c.page_shift)], c.pages);
-            page[i] = ((id * c.heads + h) << c.page_shift) + ((base + 16 * i) & (c.page_size - 1));
-        }
-        const int dk = c.d * kE8 / 8, ds = c.d / 32;  // bytes of a row, and of its scales
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int64_t row = (r < 8 ? page[0] : page[1]) + (8 * (r >> 2) + 4 * m + (r & 3)) % 16;
+    // A lane's places in a tile's rows, the same for every tile.
+    struct Lane {
+        int k[kKu], ks[kKu], v[kVu], vs[kVu];
+        int row, scales;  // bytes of a row, and of its scales
+        bool low_k, low_v;
+        __device__ __forceinline__ explicit Lane(const Cache& c) {
+            const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, d = FULL ? DC : c.d;
+            row = d * kE8 / 8;
+            scales = d / 32;
+            low_k = r < 8;
+            low_v = g < 2;
+            const int tk = (8 * (r >> 2) + (r & 3)) % 16, tv = 8 * (g & 1);
 #pragma unroll
             for (int u = 0; u < kKu; ++u) {
-                const int column = 4 * kKw * u + kKw * g;
-#pragma unroll
-                for (int i = 0; i < kKwords; ++i) k[m][u][i] = 0u;
-                if (kScaled) ks[m][u] = 127u;
-                if (column < c.d) {
-                    load_words<kKb>(c.k + row * dk + column * kE8 / 8, k[m][u]);
-                    if (kScaled) ks[m][u] = c.k_scales[row * ds + column / 32];
-                }
+                const int column = min(4 * kKw * u + kKw * g, d - kKw);
+                k[u] = tk * row + column * kE8 / 8;
+                ks[u] = tk * scales + column / 32;
             }
-        }
-        const int64_t first = (g < 2 ? page[0] : page[1]) + 8 * (g & 1);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
 #pragma unroll
             for (int u = 0; u < kVu; ++u) {
-                const int column = 16 * kVw * u + kVw * r;
-#pragma unroll
-                for (int i = 0; i < kVwords; ++i) v[j][u][i] = 0u;
-                if (kScaled) vs[j][u] = 127u;
-                if (column < c.d) {
-                    load_words<kVb>(c.v + (first + j) * dk + column * kE8 / 8, v[j][u]);
-                    if (kScaled) vs[j][u] = c.v_scales[(first + j) * ds + column / 32];
-                }
+                const int column = min(16 * kVw * u + kVw * r, d - kVw);
+                v[u] = tv * row + column * kE8 / 8;
+                vs[u] = tv * scales + column / 32;
             }
+        }
+    };
+
+    __device__ __forceinline__ void load(const Cache& c, const Lane& l, const Rows& rows) {
+        const int row = FULL ? DC * kE8 / 8 : l.row, scales = FULL ? DC / 32 : l.scales;
+        const uint8_t* const kp = l.low_k ? c.k + rows.at[0] * row : c.k + rows.at[1] * row;
+        const uint8_t* const vp = l.low_v ? c.v + rows.at[0] * row : c.v + rows.at[1] * row;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int u = 0; u < kKu; ++u) load_words<kKb>(kp + l.k[u] + 4 * m * row, k[m][u]);
+        if constexpr (kScaled) {
+            const uint8_t* const sp = l.low_k ? c.k_scales + rows.at[0] * scales : c.k_scales + rows.at[1] * scales;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int u = 0; u < kKu; ++u) ks[m][u] = sp[l.ks[u] + 4 * m * scales];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int u = 0; u < kVu; ++u) load_words<kVb>(vp + l.v[u] + j * row, v[j][u]);
+        if constexpr (kScaled) {
+            const uint8_t* const sp = l.low_v ? c.v_scales + rows.at[0] * scales : c.v_scales + rows.at[1] * scales;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < kVu; ++u) vs[j][u] = sp[l.vs[u] + j * scales];
         }
     }
 
@@ -180,12 +211,12 @@ struct Tile {
         const int token = t * kTileTokens + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (token + j >= from && token + j < end) continue;
+            const bool counts = token + j >= from && token + j < end;
 #pragma unroll
             for (int u = 0; u < kVu; ++u) {
 #pragma unroll
-                for (int i = 0; i < kVwords; ++i) v[j][u][i] = 0u;
-                if (kScaled) vs[j][u] = 127u;
+                for (int i = 0; i < kVwords; ++i) v[j][u][i] = counts ? v[j][u][i] : 0u;
+                if (kScaled) vs[j][u] = counts ? vs[j][u] : 127u;
             }
         }
     }
@@ -222,40 +253,62 @@ __device__ __forceinline__ void unrolled(Fn f) {
 }
 
 // The column of O^T's tile n, row i.
-template <CacheFormat F, int DC>
+template <class T>
 __device__ __forceinline__ int value_column(int n, int i) {
-    constexpr int w = Tile<F, DC>::kVw;
+    constexpr int w = T::kVw;
     return 16 * w * (n / w) + w * i + n % w;
 }
 
-template <CacheFormat F, int DC, bool B16>
-__global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnParams p) {
-    typedef Tile<F, DC> T;
+#define KQ_INLINE __attribute__((always_inline))
+
+template <CacheFormat F, int DC, bool B16, bool FULL>
+__global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_kernel(AttnParams p) {
+    typedef Tile<F, DC, FULL> T;
     constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
     const Cache& c = p.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const Part part = find_part(p.lengths, (int)p.B, p.max_tokens, p.window, p.parts, (int)blockIdx.x);
+    const int d = FULL ? DC : c.d;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const Part part = find_part(p.lengths, (int)p.B, p.max_tokens, p.window, p.inverse, (int)blockIdx.x);
     if (part.b < 0) return;
     const int row_tiles = (p.group + kRowTile - 1) / kRowTile;
     const int h = blockIdx.y / row_tiles, first_row = (blockIdx.y - h * row_tiles) * kRowTile;
     const int rows = min(p.group - first_row, kRowTile), head = h * p.group + first_row;
-    if (part.index == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        p.plan[2 * part.b] = part.slot;
-        p.plan[2 * part.b + 1] = part.count;
-    }
     const int32_t* const table = p.table + part.b * p.table_stride;
+    const typename T::Lane lanes(c);
+    auto where = [&](int t) KQ_INLINE { return Rows(c, table, h, t, part.end); };
+
+    const int last = part.tile + part.tiles;
+    int t = part.tile + wave;
+    T tile, ahead;
+    if (t < last) tile.load(c, lanes, where(t));
 
     bf16x8 q[T::kSteps][kQ];
-    unrolled<0, T::kSteps>([&](auto step) {
+    unrolled<0, T::kSteps>([&](auto step) KQ_INLINE {
         constexpr int u = step / T::kKs, w = step % T::kKs;
         const int column = 4 * T::kKw * u + T::kKw * g + 8 * w;
-        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (r < rows && column < c.d) {
-            const int64_t at = part.b * p.q_seq + (head + r) * p.q_head + column;
+        const int64_t at = part.b * p.q_seq + (head + min(r, rows - 1)) * p.q_head + min(column, d - 8);
+        float f[8];
+        if constexpr (B16) {
+            typedef uint32_t W __attribute__((ext_vector_type(4), aligned(2)));
+            const W w = *reinterpret_cast<const W*>(static_cast<const uint16_t*>(p.q) + at);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                f[k] = B16 ? bf16_low(static_cast<const uint16_t*>(p.q)[at + k]) : static_cast<const float*>(p.q)[at + k];
+            for (int k = 0; k < 4; ++k) {
+                f[2 * k] = bf16_low(w[k]);
+                f[2 * k + 1] = bf16_high(w[k]);
+            }
+        } else {
+            typedef float W __attribute__((ext_vector_type(4), aligned(4)));
+            const W a = *reinterpret_cast<const W*>(static_cast<const float*>(p.q) + at);
+            const W b = *reinterpret_cast<const W*>(static_cast<const float*>(p.q) + at + 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                f[k] = a[k];
+                f[4 + k] = b[k];
+            }
         }
+        const bool live = r < rows && (FULL || column < d);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = live ? f[k] : 0.f;
         split_terms<kQ>(f, q[step]);
     });
 
@@ -264,17 +317,13 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
     for (int n = 0; n < T::kVc; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     float most = kLowest, sum = 0.f;
     const float scale = p.scale * 1.44269504088896341f;  // scores in powers of two
-    for (int i = wave; i < part.tiles; i += kAttnWaves) {
-        const int t = part.tile + i;
-        T tile;
-        tile.load(c, table, h, t, part.end);
-        const bool edge = t * kTileTokens < part.first || (t + 1) * kTileTokens > part.end;
-        if (edge) tile.clear(t, part.first, part.end);
+
+    auto attend = [&](T& tile, int t) KQ_INLINE {
         float s[8];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             f32x4 a = {0.f, 0.f, 0.f, 0.f};
-            unrolled<0, T::kSteps>([&](auto step) {
+            unrolled<0, T::kSteps>([&](auto step) KQ_INLINE {
                 constexpr int u = step / T::kKs, w = step % T::kKs;
                 const bf16x8 k = tile.template keys<w>(m, u);
 #pragma unroll
@@ -283,15 +332,15 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[4 * m + k] = a[k] * scale;
         }
-        if (edge) {
+        if (t * kTileTokens < part.first || (t + 1) * kTileTokens > part.end) {
+            asm volatile("");  // a branch: tiles in between skip this
+            tile.clear(t, part.first, part.end);
             const int token = t * kTileTokens + 8 * g;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (token + k < part.first || token + k >= part.end) s[k] = -INFINITY;
         }
-        float top = s[0];
-#pragma unroll
-        for (int k = 1; k < 8; ++k) top = fmaxf(top, s[k]);
+        float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
         top = fmaxf(query_max(top), most);
         if (__any(top > most)) {
             const float f = __builtin_amdgcn_exp2f(most - top);
@@ -302,15 +351,13 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
         }
         float e[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            e[k] = __builtin_amdgcn_exp2f(s[k] - most);
-            sum += e[k];
-        }
+        for (int k = 0; k < 8; ++k) e[k] = __builtin_amdgcn_exp2f(s[k] - most);
+        sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         bf16x8 pt[kP];
         split_terms<kP>(e, pt);
 #pragma unroll
         for (int u = 0; u < T::kVu; ++u) {
-            unrolled<0, T::kVw / 2>([&](auto pair) {
+            unrolled<0, T::kVw / 2>([&](auto pair) KQ_INLINE {
                 bf16x8 a[2];
                 tile.template values<pair>(u, a);
 #pragma unroll
@@ -321,6 +368,20 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
                 }
             });
         }
+    };
+    // the next tile's loads are in flight while a tile is worked on
+    while (t < last) {
+        const int t1 = t + kAttnWaves, t2 = t1 + kAttnWaves;
+        if (t1 < last) ahead.load(c, lanes, where(t1));
+        attend(tile, t);
+        if (t1 >= last) break;
+        if (t2 < last) tile.load(c, lanes, where(t2));
+        attend(ahead, t1);
+        t = t2;
+    }
+    if (part.index == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        p.plan[2 * part.b] = part.slot;
+        p.plan[2 * part.b + 1] = part.count;
     }
 
     // The waves' results in one: the common maximum first, then sums.
@@ -344,9 +405,9 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
             for (int n = 0; n < T::kVc; ++n)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int column = value_column<F, DC>(n, 4 * g + k);
-                    if (column >= c.d) continue;
-                    float& v = shared[((wave & 1) * rows + r) * c.d + column];
+                    const int column = value_column<T>(n, 4 * g + k);
+                    if (!FULL && column >= d) continue;
+                    float& v = shared[((wave & 1) * rows + r) * d + column];
                     v = turn ? v + o[n][k] * f : o[n][k] * f;
                 }
         }
@@ -354,10 +415,10 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
     }
     const bool whole = part.count == 1;
     const int64_t place = (part.slot + part.index) * (int64_t)(c.heads * p.group) + head;  // of a part's results
-    for (int i = threadIdx.x; i < rows * c.d; i += kAttnThreads) {
-        const int row = i / c.d, column = i - row * c.d;
+    for (int i = threadIdx.x; i < rows * d; i += kAttnThreads) {
+        const int row = i / d, column = i - row * d;
         float top = stats[0][0][row], total = 0.f;
-        float v = shared[row * c.d + column] + shared[(rows + row) * c.d + column];
+        float v = shared[row * d + column] + shared[(rows + row) * d + column];
 #pragma unroll
         for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stats[0][w][row]);
 #pragma unroll
@@ -371,7 +432,7 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
                 p.lse[part.b * (int64_t)(c.heads * p.group) + head + row] =
                     total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945309f : -INFINITY;
         } else {
-            p.partial[(place + row) * c.d + column] = v;
+            p.partial[(place + row) * d + column] = v;
             if (column == 0) {
                 p.stats[2 * (place + row)] = top;
                 p.stats[2 * (place + row) + 1] = total;
@@ -425,8 +486,13 @@ int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 
 template <CacheFormat F, int DC>
 void launch_attn_of(const AttnParams& p, dim3 grid, size_t lds, hipStream_t st) {
-    if (p.is16) attn_kernel<F, DC, true><<<grid, kAttnThreads, lds, st>>>(p);
-    else attn_kernel<F, DC, false><<<grid, kAttnThreads, lds, st>>>(p);
+    if (p.c.d == DC) {
+        if (p.is16) attn_kernel<F, DC, true, true><<<grid, kAttnThreads, lds, st>>>(p);
+        else attn_kernel<F, DC, false, true><<<grid, kAttnThreads, lds, st>>>(p);
+    } else {
+        if (p.is16) attn_kernel<F, DC, true, false><<<grid, kAttnThreads, lds, st>>>(p);
+        else attn_kernel<F, DC, false, false><<<grid, kAttnThreads, lds, st>>>(p);
+    }
 }
 
 template <CacheFormat F>
@@ -446,6 +512,7 @@ int64_t attn_workspace(int64_t B, int64_t heads, int64_t group, int64_t d) {
 hipError_t launch_attn(AttnParams p, hipStream_t st) {
     const int heads = p.c.heads * p.group, row_tiles = (p.group + kRowTile - 1) / kRowTile;
     p.parts = attn_parts(p.c.heads, p.group);
+    p.inverse = 1.0 / p.parts;
     p.slots = part_slots(p.parts, p.B);
     p.plan = reinterpret_cast<int32_t*>(p.workspace);
     p.stats = reinterpret_cast<float*>(p.workspace + round16(8 * p.B));

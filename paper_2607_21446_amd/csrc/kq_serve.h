@@ -82,6 +82,7 @@ struct AttnParams {
     // filled in by the launcher: parts that a head's sequences are cut into at most, beside one each; the places of the
     // parts' results in the workspace
     int parts;
+    double inverse;  // 1 / parts
     int64_t slots;
     int32_t* plan;   // [B, 2]: first slot and number of parts
     float* stats;    // [slots, heads * group, 2]: maximum and sum

@@ -32,12 +32,14 @@ struct Span {
     }
 };
 
-__host__ __device__ __forceinline__ int64_t part_tiles(int64_t total, int parts) {
-    const int64_t c = (total + parts - 1) / parts;
-    return c > kLeastTiles ? c : kLeastTiles;
+// Tiles of a part, at least total / parts; `inverse` is 1 / parts.  No sequence has 2^26 tiles.
+__host__ __device__ __forceinline__ int part_tiles(uint64_t total, double inverse) {
+    const double c = (double)total * inverse * (1.0 + 0x1p-50);  // (total < 2^46: the product's errors are below that factor's)
+    const int n = c < 0x1p26 ? (int)c + ((double)(int)c < c) : 1 << 26;
+    return n > kLeastTiles ? n : kLeastTiles;
 }
-__host__ __device__ __forceinline__ int part_count(int tiles, int64_t c) {
-    return tiles <= c ? 1 : (int)((tiles + c - 1) / c);
+__host__ __device__ __forceinline__ int part_count(int tiles, int c) {
+    return tiles <= c ? 1 : (int)((uint32_t)(tiles + c - 1) / (uint32_t)c);
 }
 // Places for the results of parts.
 __host__ __device__ __forceinline__ int64_t part_slots(int64_t parts, int64_t B) {
@@ -62,41 +64,59 @@ struct Part {
     int tile, tiles;      // its tiles from `tile` on, tile 0 starting at token 0
 };
 
-// Part `x` of the call, found by each of a workgroup's waves: two passes over the lengths, 64 at a time.
-__device__ __forceinline__ Part find_part(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, int parts, int x) {
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_sum(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+// The sum of the lanes up to and with each.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    v = dpp_sum<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8: sums up to the lane in its row of 16
+    v = dpp_sum<0x112, 0xf>(v);
+    v = dpp_sum<0x114, 0xf>(v);
+    v = dpp_sum<0x118, 0xf>(v);
+    v = dpp_sum<0x142, 0xa>(v);  // rows 0 and 2 onto 1 and 3, then 1 onto 2 and 3
+    return dpp_sum<0x143, 0xc>(v);
+}
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// Part `x` of the call, found by each of a workgroup's waves: two passes over the lengths, 64 at a time (their tiles
+// together are below 2^32); one where there are no more than 64.
+__device__ __forceinline__ Part find_part(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, double inverse, int x) {
     const int lane = threadIdx.x & 63;
-    auto span = [&](int b) { return Span(b < B ? lengths[b] : 0, max_tokens, window); };
-    int64_t total = 0;
-    for (int b = lane; b < B; b += 64) total += span(b).tiles();
-    for (int k = 1; k < 64; k <<= 1) total += __shfl_xor((long long)total, k);
-    const int64_t c = part_tiles(total, parts);
+    auto span = [&](int b) __attribute__((always_inline)) { return Span(b < B ? lengths[b] : 0, max_tokens, window); };
+    Span s = span(lane);
+    uint64_t total = 0;
+    for (int b0 = 0;;) {
+        total += (uint32_t)lane_value((int)wave_scan((uint32_t)s.tiles()), 63);
+        b0 += 64;
+        if (b0 >= B) break;
+        s = span(b0 + lane);
+    }
+    const int c = part_tiles(total, inverse);
     Part p{-1, 0, 0, 0, 0, 0, 0, 0};
     int before = 0, slot = 0;
-    for (int b0 = 0; b0 < B; b0 += 64) {
-        const Span s = span(b0 + lane);
-        const int n = b0 + lane < B ? part_count(s.tiles(), c) : 0;
-        int upto = n, several = n > 1 ? n : 0;
-        for (int k = 1; k < 64; k <<= 1) {
-            const int u = __shfl_up(upto, k), v = __shfl_up(several, k);
-            upto += lane >= k ? u : 0;
-            several += lane >= k ? v : 0;
-        }
+    if (B > 64) s = span(lane);
+    for (int b0 = 0; b0 < B;) {
+        const int tiles = s.tiles(), n = b0 + lane < B ? part_count(tiles, c) : 0;
+        const int upto = (int)wave_scan((uint32_t)n), several = (int)wave_scan(n > 1 ? (uint32_t)n : 0u);
         const uint64_t here = __ballot(before + upto > x);
         if (here) {
             const int at = __ffsll((unsigned long long)here) - 1;
             p.b = b0 + at;
-            p.count = __builtin_amdgcn_readlane(n, at);
-            p.index = x - (before + __builtin_amdgcn_readlane(upto, at) - p.count);
-            p.slot = slot + __builtin_amdgcn_readlane(several, at) - (p.count > 1 ? p.count : 0);
-            p.first = __builtin_amdgcn_readlane(s.first, at);
-            p.end = __builtin_amdgcn_readlane(s.end, at);
-            const int64_t done = p.index * c, all = Span(p.end, max_tokens, window).tiles();
-            p.tile = p.first / kTileTokens + (int)done;
-            p.tiles = (int)(all - done < c ? all - done : c);
+            p.count = lane_value(n, at);
+            p.index = x - (before + lane_value(upto, at) - p.count);
+            p.slot = slot + lane_value(several, at) - (p.count > 1 ? p.count : 0);
+            p.first = lane_value(s.first, at);
+            p.end = lane_value(s.end, at);
+            const int done = p.index * c, left = lane_value(tiles, at) - done;
+            p.tile = p.first / kTileTokens + done;
+            p.tiles = left < c ? left : c;
             return p;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
-        slot += __builtin_amdgcn_readlane(several, 63);
+        before += lane_value(upto, 63);
+        slot += lane_value(several, 63);
+        b0 += 64;
+        s = span(b0 + lane);
     }
     return p;
 }

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 #include <ucontext.h>
 
@@ -33,12 +34,17 @@ struct ThreadIdx {
 };
 static ThreadIdx threadIdx;
 
-template <class T>
-static T shfl_xor(T v, int k) { return (T)wave::share((int64_t)v)[wave::lane ^ k]; }
-static int shfl_up(int v, int k) {
+// Lanes that no enabled row or no source lane writes keep `old`.
+static int dpp(int old, int v, int ctrl, int rows) {
     const int64_t* const s = wave::share(v);
-    return (int)s[wave::lane >= k ? wave::lane - k : wave::lane];
+    const int l = wave::lane, row = l / 16;
+    if (!(rows >> row & 1)) return old;
+    if (ctrl > 0x110 && ctrl < 0x120) return l % 16 >= ctrl - 0x110 ? (int)s[l - (ctrl - 0x110)] : old;  // row_shr
+    if (ctrl == 0x142) return row ? (int)s[16 * row - 1] : old;                                         // row_bcast 15
+    if (ctrl == 0x143) return row >= 2 ? (int)s[31] : old;                                              // row_bcast 31
+    abort();
 }
+#define __builtin_amdgcn_update_dpp(old, v, ctrl, rows, banks, bound) dpp(old, v, ctrl, rows)
 static int readlane(int v, int l) { return (int)wave::share(v)[l]; }
 static uint64_t ballot(bool b) {
     const int64_t* const s = wave::share(b);
@@ -46,8 +52,6 @@ static uint64_t ballot(bool b) {
     for (int l = 0; l < wave::kLanes; ++l) m |= (uint64_t)(s[l] != 0) << l;
     return m;
 }
-#define __shfl_xor shfl_xor
-#define __shfl_up shfl_up
 #define __ballot ballot
 #define __ffsll(v) __builtin_ffsll((long long)(v))
 #define __builtin_amdgcn_readlane readlane
@@ -61,7 +65,7 @@ kq::Part result[wave::kLanes];
 
 void lane_main() {
     const int l = wave::lane;
-    result[l] = kq::find_part(lengths.data(), (int)B, max_tokens, window, (int)parts, (int)block);
+    result[l] = kq::find_part(lengths.data(), (int)B, max_tokens, window, 1.0 / parts, (int)block);
 }
 }  // namespace
 

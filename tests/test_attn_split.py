@@ -43,7 +43,11 @@ def _span(n, max_tokens, window):
 def _check(lengths, max_tokens, window, parts, got):
     """got: of every block of the grid, in order."""
     spans = [_span(n, max_tokens, window) for n in lengths]
-    c = max(LEAST, -(-sum(t for _, _, t in spans) // parts))
+    # tiles of a part: total / parts or, where rounding takes an even quotient up, one more
+    total = sum(t for _, _, t in spans)
+    c, ways = max(LEAST, -(-total // parts)), [p[2] for p in filter(None, got)]
+    if total % parts == 0 and len(ways) == sum(max(1, -(-t // (c + 1))) for _, _, t in spans) != sum(max(1, -(-t // c)) for _, _, t in spans):
+        c += 1
     found, slots = {b: [] for b in range(len(lengths))}, []
     for p in filter(None, got):
         b, index, count, slot, first, end, tile, tiles = p
