@@ -2,8 +2,8 @@
 //     out = softmax(scale q K^T) V
 // over the sequence's tokens (or its last `window`), K and V in bf16, MXFP8 or
 // MXFP4.  One pass over the cache with the running maximum and sum of the
-// softmax; ragged sequences are cut into parts of equal length (kq_split.h) and
-// joined by a second launch.
+// softmax; ragged sequences are shared out to workgroups in runs of equal length
+// (kq_split.h), and those that are cut are joined by a second launch.
 //
 // A wave takes a tile of 32 tokens of one head of the cache and up to 16 of the
 // query heads that share it.  Both products run on the bf16 matrix cores, which
@@ -37,7 +37,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kAttnWaves = 4;
 constexpr int kAttnThreads = 64 * kAttnWaves;
-constexpr int kAttnGroups = 1024;  // workgroups that a call's parts are cut for
+constexpr int kMostGroups = 1280;  // workgroups of a launch, where each has its run
 constexpr int kRowTile = 16;       // query heads of a workgroup
 
 template <CacheFormat F>
@@ -262,31 +262,40 @@ __device__ __forceinline__ int value_column(int n, int i) {
 #define KQ_INLINE __attribute__((always_inline))
 
 template <CacheFormat F, int DC, bool B16, bool FULL>
-__global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnParams p) {
     typedef Tile<F, DC, FULL> T;
     constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
+    constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;  // tiles that a wave has loaded or is loading
+    extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3
+    __shared__ float stats[2][kAttnWaves][kRowTile];
     const Cache& c = p.c;
     const int d = FULL ? DC : c.d;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const Part part = find_part(p.lengths, (int)p.B, p.max_tokens, p.window, p.inverse, (int)blockIdx.x);
-    if (part.b < 0) return;
+    Run run = find_run(p.lengths, (int)p.B, p.max_tokens, p.window, p.inverse, (int)blockIdx.x);
     const int row_tiles = (p.group + kRowTile - 1) / kRowTile;
     const int h = blockIdx.y / row_tiles, first_row = (blockIdx.y - h * row_tiles) * kRowTile;
     const int rows = min(p.group - first_row, kRowTile), head = h * p.group + first_row;
-    const int32_t* const table = p.table + part.b * p.table_stride;
+    const int64_t heads = (int64_t)c.heads * p.group;
     const typename T::Lane lanes(c);
-    auto where = [&](int t) KQ_INLINE { return Rows(c, table, h, t, part.end); };
-
-    const int last = part.tile + part.tiles;
-    int t = part.tile + wave;
-    T tile, ahead;
-    if (t < last) tile.load(c, lanes, where(t));
+    for (; run.tiles > 0; ++run.b, run.skip = 0) {
+    // a piece: a sequence's tiles in this run
+    const Span span(((const_i32_ptr)p.lengths)[run.b], p.max_tokens, p.window);
+    const int left = span.tiles() - run.skip, tiles = left < run.tiles ? left : (int)run.tiles;
+    run.tiles -= tiles;
+    const int32_t* const table = p.table + run.b * p.table_stride;
+    auto where = [&](int t) KQ_INLINE { return Rows(c, table, h, t, span.end); };
+    const int last = span.end > span.first ? span.first_tile() + run.skip + tiles : 0;
+    int t = span.first_tile() + run.skip + wave;
+    T tile[kAhead];
+    unrolled<0, kAhead - 1>([&](auto stage) KQ_INLINE {
+        if (t + stage * kAttnWaves < last) tile[stage].load(c, lanes, where(t + stage * kAttnWaves));
+    });
 
     bf16x8 q[T::kSteps][kQ];
     unrolled<0, T::kSteps>([&](auto step) KQ_INLINE {
         constexpr int u = step / T::kKs, w = step % T::kKs;
         const int column = 4 * T::kKw * u + T::kKw * g + 8 * w;
-        const int64_t at = part.b * p.q_seq + (head + min(r, rows - 1)) * p.q_head + min(column, d - 8);
+        const int64_t at = run.b * p.q_seq + (head + min(r, rows - 1)) * p.q_head + min(column, d - 8);
         float f[8];
         if constexpr (B16) {
             typedef uint32_t W __attribute__((ext_vector_type(4), aligned(2)));
@@ -332,13 +341,13 @@ __global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_ke
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[4 * m + k] = a[k] * scale;
         }
-        if (t * kTileTokens < part.first || (t + 1) * kTileTokens > part.end) {
+        if (t * kTileTokens < span.first || (t + 1) * kTileTokens > span.end) {
             asm volatile("");  // a branch: tiles in between skip this
-            tile.clear(t, part.first, part.end);
+            tile.clear(t, span.first, span.end);
             const int token = t * kTileTokens + 8 * g;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (token + k < part.first || token + k >= part.end) s[k] = -INFINITY;
+                if (token + k < span.first || token + k >= span.end) s[k] = -INFINITY;
         }
         float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
         top = fmaxf(query_max(top), most);
@@ -369,33 +378,27 @@ __global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_ke
             });
         }
     };
-    // the next tile's loads are in flight while a tile is worked on
+    // the next tiles' loads are in flight while a tile is worked on
     while (t < last) {
-        const int t1 = t + kAttnWaves, t2 = t1 + kAttnWaves;
-        if (t1 < last) ahead.load(c, lanes, where(t1));
-        attend(tile, t);
-        if (t1 >= last) break;
-        if (t2 < last) tile.load(c, lanes, where(t2));
-        attend(ahead, t1);
-        t = t2;
+        bool more = true;
+        unrolled<0, kAhead>([&](auto stage) KQ_INLINE {
+            constexpr int now = stage, late = (stage + kAhead - 1) % kAhead;
+            if (!more) return;
+            const int tn = t + (kAhead - 1) * kAttnWaves;
+            if (tn < last) tile[late].load(c, lanes, where(tn));
+            attend(tile[now], t);
+            t += kAttnWaves;
+            more = t < last;
+        });
     }
-    if (part.index == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        p.plan[2 * part.b] = part.slot;
-        p.plan[2 * part.b + 1] = part.count;
-    }
-
-    // The waves' results in one: the common maximum first, then sums.
-    extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3
-    __shared__ float stats[2][kAttnWaves][kRowTile];
+    // the waves' results in one: the common maximum first, then sums
     sum = query_sum(sum);
     if (g == 0) {
         stats[0][wave][r] = most;
         stats[1][wave][r] = sum;
     }
     __syncthreads();
-    float all = stats[0][0][r];
-#pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) all = fmaxf(all, stats[0][w][r]);
+    float all = fmaxf(fmaxf(stats[0][0][r], stats[0][1][r]), fmaxf(stats[0][2][r], stats[0][3][r]));
     const float f = __builtin_amdgcn_exp2f(most - all);
     static_assert(kAttnWaves == 4, "two waves a place");
 #pragma unroll
@@ -413,23 +416,28 @@ __global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_ke
         }
         __syncthreads();
     }
-    const bool whole = part.count == 1;
-    const int64_t place = (part.slot + part.index) * (int64_t)(c.heads * p.group) + head;  // of a part's results
+    // a sequence in one run is done; one that is cut leaves its piece, and its first run the place of them all
+    const bool begins = run.skip == 0, whole = begins && tiles == left;
+    if (begins && blockIdx.y == 0 && threadIdx.x == 0) {
+        const int64_t over = left - tiles;  // in the runs that follow
+        p.plan[2 * run.b] = blockIdx.x;
+        p.plan[2 * run.b + 1] = over > 0 ? 2 + (int)((over - 1) / run.each) : 1;
+    }
+    const int64_t place = (2 * (int64_t)blockIdx.x + begins) * heads + head;
     for (int i = threadIdx.x; i < rows * d; i += kAttnThreads) {
         const int row = i / d, column = i - row * d;
-        float top = stats[0][0][row], total = 0.f;
-        float v = shared[row * d + column] + shared[(rows + row) * d + column];
-#pragma unroll
-        for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stats[0][w][row]);
+        const float top = fmaxf(fmaxf(stats[0][0][row], stats[0][1][row]), fmaxf(stats[0][2][row], stats[0][3][row]));
+        float total = 0.f;
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) total += stats[1][w][row] * __builtin_amdgcn_exp2f(stats[0][w][row] - top);
+        float v = shared[row * d + column] + shared[(rows + row) * d + column];
         if (whole) {
             v = total != 0.f ? v / total : 0.f;
-            const int64_t at = part.b * p.out_seq + (head + row) * p.out_head + column;
+            const int64_t at = run.b * p.out_seq + (head + row) * p.out_head + column;
             if (B16) static_cast<__bf16*>(p.out)[at] = (__bf16)v;
             else static_cast<float*>(p.out)[at] = v;
             if (p.lse && column == 0)
-                p.lse[part.b * (int64_t)(c.heads * p.group) + head + row] =
+                p.lse[run.b * heads + head + row] =
                     total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945309f : -INFINITY;
         } else {
             p.partial[(place + row) * d + column] = v;
@@ -439,97 +447,130 @@ __global__ __launch_bounds__(kAttnThreads, B16 && DC < 256 ? 2 : 1) void attn_ke
             }
         }
     }
+    __syncthreads();  // the next piece's waves write where these read
+    }
 }
 
-// Parts' results in one, a workgroup a sequence and query head.
+// The pieces of a sequence in one, a workgroup a sequence and query head: its threads take four columns each of as many pieces
+// at once as there are threads for.
+constexpr int kJoinThreads = 256;
+
 template <bool B16>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnParams p) {
     const int b = blockIdx.x, head = blockIdx.y, d = p.c.d, heads = p.c.heads * p.group;
-    const int slot = p.plan[2 * b], count = p.plan[2 * b + 1];
+    const int run = p.plan[2 * b], count = p.plan[2 * b + 1];
     if (count <= 1) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = (int64_t)slot * heads + head;
-    float top = kLowest;
-    for (int i = lane; i < count; i += 64) top = fmaxf(top, p.stats[2 * (first + (int64_t)i * heads)]);
+    // piece 0 is at place 2 run + 1, piece i at 2 (run + i)
+    auto piece = [&](int i) KQ_INLINE { return (2 * (int64_t)(run + i) + (i == 0)) * heads + head; };
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2* const stats = reinterpret_cast<const f32x2*>(p.stats);
+    const int columns = d / 4, at = threadIdx.x / columns, column = threadIdx.x - at * columns, step = kJoinThreads / columns;
+    const f32x4* const from = reinterpret_cast<const f32x4*>(p.partial) + column;
+    // every wave has the maximum of all pieces
+    float top = kLowest, total = 0.f;
+    for (int i = lane; i < count; i += 64) top = fmaxf(top, stats[piece(i)][0]);
     for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
-    float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};  // columns lane, lane + 64, ...
-    for (int i = wave; i < count; i += 4) {
-        const int64_t at = first + (int64_t)i * heads;
-        const float f = __builtin_amdgcn_exp2f(p.stats[2 * at] - top);
-        total += f * p.stats[2 * at + 1];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (lane + 64 * k < d) v[k] += f * p.partial[at * d + lane + 64 * k];
+    if (wave == 0) {
+        for (int i = lane; i < count; i += 64) {
+            const f32x2 s = stats[piece(i)];
+            total += s[1] * __builtin_amdgcn_exp2f(s[0] - top);
+        }
+        for (int k = 1; k < 64; k <<= 1) total += __shfl_xor(total, k);
     }
-    __shared__ float sums[4], part[4][256];
-    if (lane == 0) sums[wave] = total;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = v[k];
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (at < step) {
+#pragma unroll 4
+        for (int i = at; i < count; i += step)
+            v += from[piece(i) * columns] * __builtin_amdgcn_exp2f(stats[piece(i)][0] - top);
+    }
+    __shared__ f32x4 sums[kJoinThreads];
+    __shared__ float all;
+    sums[threadIdx.x] = v;
+    if (threadIdx.x == 0) all = total;
     __syncthreads();
-    total = sums[0] + sums[1] + sums[2] + sums[3];
-    if ((int)threadIdx.x < d) {
-        const int i = threadIdx.x;
-        const float f = total != 0.f ? (part[0][i] + part[1][i] + part[2][i] + part[3][i]) / total : 0.f;
-        const int64_t at = b * p.out_seq + head * p.out_head + i;
-        if (B16) static_cast<__bf16*>(p.out)[at] = (__bf16)f;
-        else static_cast<float*>(p.out)[at] = f;
+    total = all;
+    if (at == 0) {
+        const int n = min(step, count);
+        for (int i = 1; i < n; ++i) v += sums[i * columns + column];
+        const int64_t to = b * p.out_seq + head * p.out_head + 4 * column;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = total != 0.f ? v[k] / total : 0.f;
+            if (B16) static_cast<__bf16*>(p.out)[to + k] = (__bf16)f;
+            else static_cast<float*>(p.out)[to + k] = f;
+        }
     }
     if (p.lse && threadIdx.x == 0)
         p.lse[(int64_t)b * heads + head] = total != 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.693147180559945309f : -INFINITY;
 }
 
-int attn_parts(int64_t heads, int64_t group) {
-    return (int)std::max<int64_t>(1, kAttnGroups / (heads * ((group + kRowTile - 1) / kRowTile)));
+// Runs that a head's tiles are cut into at most.
+int64_t most_runs(int64_t heads, int64_t group) {
+    return std::max<int64_t>(1, kMostGroups / (heads * ((group + kRowTile - 1) / kRowTile)));
 }
 
 int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 
+// Workgroups of a kernel that the GPU holds at once.
+template <class K>
+int resident_groups(K kernel, size_t lds) {
+    int device = 0, units = 0, each = 0;
+    if (hipGetDevice(&device) != hipSuccess || hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess ||
+        hipOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kAttnThreads, lds) != hipSuccess)
+        return 512;
+    return units * std::max(each, 1);
+}
+
+template <CacheFormat F, int DC, bool B16, bool FULL>
+hipError_t launch_attn_of(AttnParams& p, int64_t most, hipStream_t st) {
+    const size_t lds = sizeof(float) * 2 * std::min(p.group, kRowTile) * p.c.d;
+    static const int resident = resident_groups(attn_kernel<F, DC, B16, FULL>, sizeof(float) * 2 * kRowTile * DC);
+    const int rows = p.c.heads * ((p.group + kRowTile - 1) / kRowTile);
+    p.runs = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(resident / rows, most_runs(p.c.heads, p.group)), most));
+    p.inverse = 1.0 / p.runs;
+    attn_kernel<F, DC, B16, FULL><<<dim3((unsigned)p.runs, (unsigned)rows), kAttnThreads, lds, st>>>(p);
+    return hipGetLastError();
+}
+
 template <CacheFormat F, int DC>
-void launch_attn_of(const AttnParams& p, dim3 grid, size_t lds, hipStream_t st) {
-    if (p.c.d == DC) {
-        if (p.is16) attn_kernel<F, DC, true, true><<<grid, kAttnThreads, lds, st>>>(p);
-        else attn_kernel<F, DC, false, true><<<grid, kAttnThreads, lds, st>>>(p);
-    } else {
-        if (p.is16) attn_kernel<F, DC, true, false><<<grid, kAttnThreads, lds, st>>>(p);
-        else attn_kernel<F, DC, false, false><<<grid, kAttnThreads, lds, st>>>(p);
-    }
+hipError_t launch_attn_width(AttnParams& p, int64_t most, hipStream_t st) {
+    if (p.c.d == DC) return p.is16 ? launch_attn_of<F, DC, true, true>(p, most, st) : launch_attn_of<F, DC, false, true>(p, most, st);
+    return p.is16 ? launch_attn_of<F, DC, true, false>(p, most, st) : launch_attn_of<F, DC, false, false>(p, most, st);
 }
 
 template <CacheFormat F>
-void launch_attn_format(const AttnParams& p, dim3 grid, size_t lds, hipStream_t st) {
-    if (p.c.d <= 64) launch_attn_of<F, 64>(p, grid, lds, st);
-    else if (p.c.d <= 128) launch_attn_of<F, 128>(p, grid, lds, st);
-    else launch_attn_of<F, 256>(p, grid, lds, st);
+hipError_t launch_attn_format(AttnParams& p, int64_t most, hipStream_t st) {
+    if (p.c.d <= 64) return launch_attn_width<F, 64>(p, most, st);
+    if (p.c.d <= 128) return launch_attn_width<F, 128>(p, most, st);
+    return launch_attn_width<F, 256>(p, most, st);
 }
 
 }  // namespace
 
 int64_t attn_workspace(int64_t B, int64_t heads, int64_t group, int64_t d) {
-    const int64_t rows = part_slots(attn_parts(heads, group), B) * heads * group;
+    const int64_t rows = run_slots(most_runs(heads, group)) * heads * group;
     return round16(8 * B) + round16(8 * rows) + round16(4 * rows * d);
 }
 
 hipError_t launch_attn(AttnParams p, hipStream_t st) {
-    const int heads = p.c.heads * p.group, row_tiles = (p.group + kRowTile - 1) / kRowTile;
-    p.parts = attn_parts(p.c.heads, p.group);
-    p.inverse = 1.0 / p.parts;
-    p.slots = part_slots(p.parts, p.B);
+    const int heads = p.c.heads * p.group;
     p.plan = reinterpret_cast<int32_t*>(p.workspace);
     p.stats = reinterpret_cast<float*>(p.workspace + round16(8 * p.B));
-    p.partial = reinterpret_cast<float*>(p.workspace + round16(8 * p.B) + round16(8 * p.slots * heads));
-    const dim3 grid((unsigned)(p.parts + p.B), (unsigned)(p.c.heads * row_tiles));
-    const size_t lds = sizeof(float) * 2 * std::min(p.group, kRowTile) * p.c.d;
+    p.partial = reinterpret_cast<float*>(p.workspace + round16(8 * p.B) + round16(8 * run_slots(most_runs(p.c.heads, p.group)) * heads));
+    // no more runs than the longest sequences that the table holds can fill
+    const int64_t longest = (p.window > 0 ? std::min(p.window + kTileTokens - 1, p.max_tokens) : p.max_tokens) / kTileTokens + 1;
+    const int64_t most = (p.B * longest + kLeastTiles - 1) / kLeastTiles;
+    hipError_t e = hipSuccess;
     switch (p.c.format) {
-        case CacheFormat::Bf16: launch_attn_format<CacheFormat::Bf16>(p, grid, lds, st); break;
-        case CacheFormat::Mxfp8: launch_attn_format<CacheFormat::Mxfp8>(p, grid, lds, st); break;
-        case CacheFormat::Mxfp4: launch_attn_format<CacheFormat::Mxfp4>(p, grid, lds, st); break;
+        case CacheFormat::Bf16: e = launch_attn_format<CacheFormat::Bf16>(p, most, st); break;
+        case CacheFormat::Mxfp8: e = launch_attn_format<CacheFormat::Mxfp8>(p, most, st); break;
+        case CacheFormat::Mxfp4: e = launch_attn_format<CacheFormat::Mxfp4>(p, most, st); break;
     }
-    const hipError_t e = hipGetLastError();
-    // a table of no more tokens than the least part has holds no sequence of several parts
-    if (e != hipSuccess || p.max_tokens <= kLeastTiles * kTileTokens) return e;
+    if (e != hipSuccess || p.runs == 1) return e;  // (one run cuts no sequence)
     const dim3 joins((unsigned)p.B, (unsigned)heads);
-    if (p.is16) attn_join_kernel<true><<<joins, 256, 0, st>>>(p);
-    else attn_join_kernel<false><<<joins, 256, 0, st>>>(p);
+    if (p.is16) attn_join_kernel<true><<<joins, kJoinThreads, 0, st>>>(p);
+    else attn_join_kernel<false><<<joins, kJoinThreads, 0, st>>>(p);
     return hipGetLastError();
 }
 

@@ -79,14 +79,13 @@ struct AttnParams {
     int is16;                 // q and out: 1 bf16, 0 fp32
     float* lse;               // [B, heads * group] or null
     uint8_t* workspace;       // attn_workspace bytes
-    // filled in by the launcher: parts that a head's sequences are cut into at most, beside one each; the places of the
-    // parts' results in the workspace
-    int parts;
-    double inverse;  // 1 / parts
-    int64_t slots;
-    int32_t* plan;   // [B, 2]: first slot and number of parts
-    float* stats;    // [slots, heads * group, 2]: maximum and sum
-    float* partial;  // [slots, heads * group, d]
+    // filled in by the launcher: runs that a head's tiles are cut into, and the places of their pieces' results in the
+    // workspace
+    int runs;
+    double inverse;  // 1 / runs
+    int32_t* plan;   // [B, 2]: a sequence's first run, and how many it has pieces in
+    float* stats;    // [run_slots, heads * group, 2]: maximum and sum
+    float* partial;  // [run_slots, heads * group, d]
 };
 int64_t attn_workspace(int64_t B, int64_t heads, int64_t group, int64_t d);
 hipError_t launch_attn(AttnParams p, hipStream_t st);

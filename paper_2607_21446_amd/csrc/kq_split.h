@@ -1,12 +1,14 @@
-// How attention over a cache (kq_attn.hip) cuts ragged sequences into parts of
-// equal length, from lengths that are on the device only.
+// How attention over a cache (kq_attn.hip) shares ragged sequences out to its
+// workgroups, from lengths that are on the device only.
 //
-// Tokens count in tiles of 32.  All sequences' tiles T together are cut into
-// parts of c = max(least, ceil(T / parts)) tiles, a sequence's last part
-// shorter; an empty sequence has one part.  So there are at most
-// parts + B parts, and at most 2 parts of them belong to sequences of several
-// (a sequence of t > c tiles has ceil(t / c) < 2 t / c): the grid and the
-// places for their results are sized by that, whatever the lengths are.
+// Tokens count in tiles of 32, an empty sequence as one.  All sequences' tiles
+// in a row, T of them, are cut into runs of c = max(least, ceil(T / runs)),
+// one for each workgroup of a head: all have the same work, whatever the
+// lengths are.  A run is pieces of sequences.  A sequence inside one run is
+// done by its workgroup; one that is cut has pieces in runs x0 .. x1, whose
+// results go to places 2 x0 + 1, 2 (x0 + 1), 2 (x0 + 2) ..: a run has at most
+// one piece that begins inside its sequence (its first) and one that ends
+// there (its last).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -16,7 +18,7 @@ namespace kq {
 namespace {
 
 constexpr int kTileTokens = 32;
-constexpr int kLeastTiles = 4;  // of a part: a tile for each of a workgroup's waves
+constexpr int kLeastTiles = 4;  // of a run: a tile for each of a workgroup's waves
 
 // The tokens of a sequence that count: first .. end - 1; tiles start at multiples of 32.
 struct Span {
@@ -27,24 +29,20 @@ struct Span {
         first = window > 0 && window < n ? (int)(n - window) : 0;
     }
     __host__ __device__ __forceinline__ int first_tile() const { return first / kTileTokens; }
+    // An empty sequence has one, which holds no token that counts.
     __host__ __device__ __forceinline__ int tiles() const {
-        return end > first ? (end - 1) / kTileTokens + 1 - first_tile() : 0;
+        return end > first ? (end - 1) / kTileTokens + 1 - first_tile() : 1;
     }
 };
 
-// Tiles of a part, at least total / parts; `inverse` is 1 / parts.  No sequence has 2^26 tiles.
-__host__ __device__ __forceinline__ int part_tiles(uint64_t total, double inverse) {
+// Tiles of a run, at least total / runs; `inverse` is 1 / runs.  The result is below 2^31: runs past it stay empty.
+__host__ __device__ __forceinline__ int64_t run_tiles(uint64_t total, double inverse) {
     const double c = (double)total * inverse * (1.0 + 0x1p-50);  // (total < 2^46: the product's errors are below that factor's)
-    const int n = c < 0x1p26 ? (int)c + ((double)(int)c < c) : 1 << 26;
+    const int64_t n = (int64_t)c + ((double)(int64_t)c < c);
     return n > kLeastTiles ? n : kLeastTiles;
 }
-__host__ __device__ __forceinline__ int part_count(int tiles, int c) {
-    return tiles <= c ? 1 : (int)((uint32_t)(tiles + c - 1) / (uint32_t)c);
-}
-// Places for the results of parts.
-__host__ __device__ __forceinline__ int64_t part_slots(int64_t parts, int64_t B) {
-    return 2 * parts < parts + B ? 2 * parts : parts + B;
-}
+// Places for the results of pieces.
+__host__ __device__ __forceinline__ int64_t run_slots(int64_t runs) { return 2 * runs; }
 
 // Which of a sequence's pages holds token `token`; tokens from `end` (at least 1) on are looked up in the last one.
 __host__ __device__ __forceinline__ int page_index(int token, int end, int page_shift) {
@@ -56,12 +54,12 @@ __host__ __device__ __forceinline__ int64_t page_of(int32_t entry, int64_t pages
     return entry < 0 ? 0 : entry < pages ? entry : pages - 1;
 }
 
-// A workgroup's part; b < 0: none.
-struct Part {
-    int b, index, count;  // sequence, number in it and how many it has
-    int slot;             // place of the sequence's first result, if it has several parts
-    int first, end;       // its tokens that count
-    int tile, tiles;      // its tiles from `tile` on, tile 0 starting at token 0
+// A workgroup's run: from tile `skip` of sequence b on, `tiles` in all (0: none).
+struct Run {
+    int b;
+    int skip;
+    int64_t tiles;
+    int64_t each;  // of every run
 };
 
 template <int CTRL, int ROWS>
@@ -79,46 +77,40 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 }
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// Part `x` of the call, found by each of a workgroup's waves: two passes over the lengths, 64 at a time (their tiles
-// together are below 2^32); one where there are no more than 64.
-__device__ __forceinline__ Part find_part(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, double inverse, int x) {
+// Run x, found by each of a workgroup's waves: two passes over the lengths, 64 at a time (their tiles together are below
+// 2^32); one where there are no more than 64.
+__device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, double inverse, int x) {
     const int lane = threadIdx.x & 63;
-    auto span = [&](int b) __attribute__((always_inline)) { return Span(b < B ? lengths[b] : 0, max_tokens, window); };
-    Span s = span(lane);
+    auto tiles = [&](int b) __attribute__((always_inline)) { return b < B ? (uint32_t)Span(lengths[b], max_tokens, window).tiles() : 0u; };
+    uint32_t n = tiles(lane), upto;
     uint64_t total = 0;
     for (int b0 = 0;;) {
-        total += (uint32_t)lane_value((int)wave_scan((uint32_t)s.tiles()), 63);
+        upto = wave_scan(n);
+        total += (uint32_t)lane_value((int)upto, 63);
         b0 += 64;
         if (b0 >= B) break;
-        s = span(b0 + lane);
+        n = tiles(b0 + lane);
     }
-    const int c = part_tiles(total, inverse);
-    Part p{-1, 0, 0, 0, 0, 0, 0, 0};
-    int before = 0, slot = 0;
-    if (B > 64) s = span(lane);
-    for (int b0 = 0; b0 < B;) {
-        const int tiles = s.tiles(), n = b0 + lane < B ? part_count(tiles, c) : 0;
-        const int upto = (int)wave_scan((uint32_t)n), several = (int)wave_scan(n > 1 ? (uint32_t)n : 0u);
-        const uint64_t here = __ballot(before + upto > x);
+    Run r{0, 0, 0, run_tiles(total, inverse)};
+    const uint64_t from = (uint64_t)x * (uint64_t)r.each;
+    if (from >= total) return r;
+    uint64_t before = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+        if (B > 64) {
+            n = tiles(b0 + lane);
+            upto = wave_scan(n);
+        }
+        const uint64_t here = __ballot(before + upto > from);
         if (here) {
             const int at = __ffsll((unsigned long long)here) - 1;
-            p.b = b0 + at;
-            p.count = lane_value(n, at);
-            p.index = x - (before + lane_value(upto, at) - p.count);
-            p.slot = slot + lane_value(several, at) - (p.count > 1 ? p.count : 0);
-            p.first = lane_value(s.first, at);
-            p.end = lane_value(s.end, at);
-            const int done = p.index * c, left = lane_value(tiles, at) - done;
-            p.tile = p.first / kTileTokens + done;
-            p.tiles = left < c ? left : c;
-            return p;
+            r.b = b0 + at;
+            r.skip = (int)(from - before - (uint32_t)(lane_value((int)upto, at) - lane_value((int)n, at)));
+            r.tiles = (int64_t)(total - from) < r.each ? (int64_t)(total - from) : r.each;
+            return r;
         }
-        before += lane_value(upto, 63);
-        slot += lane_value(several, 63);
-        b0 += 64;
-        s = span(b0 + lane);
+        before += (uint32_t)lane_value((int)upto, 63);
     }
-    return p;
+    return r;
 }
 
 }  // namespace

@@ -1,11 +1,10 @@
 // csrc/kq_split.h on the CPU: one wave's 64 lanes as coroutines that meet at every operation across
-// lanes.  Reads cases from stdin: "B max_tokens window parts lengths... blocks..." with the number of
-// blocks before them, prints for every block "-" (no part) or "b index count slot first end tile tiles".
+// lanes.  Reads cases from stdin: "B max_tokens window runs lengths... blocks..." with the number of
+// blocks before them, prints for every block "b skip tiles each".
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdio.h>
 #include <stdlib.h>
-#include <string.h>
 #include <ucontext.h>
 
 #include <memory>
@@ -60,12 +59,12 @@ static uint64_t ballot(bool b) {
 
 namespace {
 std::vector<int32_t> lengths;
-long long B, max_tokens, window, parts, block;
-kq::Part result[wave::kLanes];
+long long B, max_tokens, window, runs, block;
+kq::Run result[wave::kLanes];
 
 void lane_main() {
     const int l = wave::lane;
-    result[l] = kq::find_part(lengths.data(), (int)B, max_tokens, window, 1.0 / parts, (int)block);
+    result[l] = kq::find_run(lengths.data(), (int)B, max_tokens, window, 1.0 / runs, (int)block);
 }
 }  // namespace
 
@@ -78,7 +77,7 @@ int main(int argc, char** argv) {
     constexpr size_t kStack = 64 << 10;
     for (int l = 0; l < wave::kLanes; ++l) stack.emplace_back(new char[kStack]);
     long long blocks;
-    while (scanf("%lld %lld %lld %lld", &B, &max_tokens, &window, &parts) == 4) {
+    while (scanf("%lld %lld %lld %lld", &B, &max_tokens, &window, &runs) == 4) {
         lengths.assign(B, 0);
         for (auto& n : lengths)
             if (scanf("%d", &n) != 1) return 2;
@@ -104,11 +103,10 @@ int main(int argc, char** argv) {
                 for (int l = 1; l < wave::kLanes; ++l)
                     if (wave::turn[l] != wave::turn[0]) return 3;  // lanes that part
             } while (wave::turn[wave::kLanes - 1] != last);
-            const kq::Part& p = result[0];
+            const kq::Run& r = result[0];
             for (int l = 1; l < wave::kLanes; ++l)
-                if (memcmp(&result[l], &p, sizeof p) != 0) return 4;
-            if (p.b < 0) puts("-");
-            else printf("%d %d %d %d %d %d %d %d\n", p.b, p.index, p.count, p.slot, p.first, p.end, p.tile, p.tiles);
+                if (result[l].b != r.b || result[l].skip != r.skip || result[l].tiles != r.tiles || result[l].each != r.each) return 4;
+            printf("%d %d %lld %lld\n", r.b, r.skip, (long long)r.tiles, (long long)r.each);
         }
     }
     return 0;
