@@ -278,14 +278,16 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
     const int64_t heads = (int64_t)c.heads * p.group;
     const typename T::Lane lanes(c);
     for (; run.tiles > 0; ++run.b, run.skip = 0) {
-    // a piece: a sequence's tiles in this run
+    // a piece: a sequence's tiles in this run, from `done` on
     const Span span(((const_i32_ptr)p.lengths)[run.b], p.max_tokens, p.window);
-    const int left = span.tiles() - run.skip, tiles = left < run.tiles ? left : (int)run.tiles;
-    run.tiles -= tiles;
+    const int done = max(run.skip - kPieceTiles, 0), left = span.tiles() - done, before = max(kPieceTiles - run.skip, 0);
+    const int tiles = run.tiles < left + before ? (int)run.tiles - before : left;
+    run.tiles -= tiles + before;
+    if (tiles <= 0) break;  // the run ends before the first
     const int32_t* const table = p.table + run.b * p.table_stride;
     auto where = [&](int t) KQ_INLINE { return Rows(c, table, h, t, span.end); };
-    const int last = span.end > span.first ? span.first_tile() + run.skip + tiles : 0;
-    int t = span.first_tile() + run.skip + wave;
+    const int last = span.end > span.first ? span.first_tile() + done + tiles : 0;
+    int t = span.first_tile() + done + wave;
     T tile[kAhead];
     unrolled<0, kAhead - 1>([&](auto stage) KQ_INLINE {
         if (t + stage * kAttnWaves < last) tile[stage].load(c, lanes, where(t + stage * kAttnWaves));
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
         __syncthreads();
     }
     // a sequence in one run is done; one that is cut leaves its piece, and its first run the place of them all
-    const bool begins = run.skip == 0, whole = begins && tiles == left;
+    const bool begins = done == 0, whole = begins && tiles == left;
     if (begins && blockIdx.y == 0 && threadIdx.x == 0) {
         const int64_t over = left - tiles;  // in the runs that follow
         p.plan[2 * run.b] = blockIdx.x;
@@ -559,7 +561,7 @@ hipError_t launch_attn(AttnParams p, hipStream_t st) {
     p.stats = reinterpret_cast<float*>(p.workspace + round16(8 * p.B));
     p.partial = reinterpret_cast<float*>(p.workspace + round16(8 * p.B) + round16(8 * run_slots(most_runs(p.c.heads, p.group)) * heads));
     // no more runs than the longest sequences that the table holds can fill
-    const int64_t longest = (p.window > 0 ? std::min(p.window + kTileTokens - 1, p.max_tokens) : p.max_tokens) / kTileTokens + 1;
+    const int64_t longest = (p.window > 0 ? std::min(p.window + kTileTokens - 1, p.max_tokens) : p.max_tokens) / kTileTokens + 1 + kPieceTiles;
     const int64_t most = (p.B * longest + kLeastTiles - 1) / kLeastTiles;
     hipError_t e = hipSuccess;
     switch (p.c.format) {

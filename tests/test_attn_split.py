@@ -11,7 +11,7 @@ import pytest
 
 from conftest import ROOT
 
-TILE, LEAST, MOST = 32, 4, 2 ** 31 - 64
+TILE, LEAST, PIECE, MOST = 32, 4, 12, 2 ** 31 - 64
 
 
 @pytest.fixture(scope="module")
@@ -42,7 +42,8 @@ def _tiles(n, max_tokens, window):
 
 
 def _check(lengths, max_tokens, window, runs, got):
-    all_ = [_tiles(n, max_tokens, window) for n in lengths]
+    # PIECE tiles before a sequence's own stand for what a piece costs beside them
+    all_ = [_tiles(n, max_tokens, window) + PIECE for n in lengths]
     total = sum(all_)
     each = got[0][3]
     # total / runs or, where rounding takes an even quotient up, one more
@@ -51,7 +52,7 @@ def _check(lengths, max_tokens, window, runs, got):
     begin = [0]
     for t in all_:
         begin.append(begin[-1] + t)
-    places = []
+    places, seen = [], [0] * len(lengths)
     for x, (b, skip, tiles, _) in enumerate(got):
         assert tiles == max(0, min(each, total - x * each)), (x, tiles)
         if not tiles:
@@ -59,12 +60,17 @@ def _check(lengths, max_tokens, window, runs, got):
         assert 0 <= b < len(lengths) and 0 <= skip < all_[b] and begin[b] + skip == x * each, (x, b, skip)
         while tiles:  # its pieces, as the kernel walks through them
             n = min(all_[b] - skip, tiles)
-            if n < all_[b]:
-                places.append(2 * x + (skip == 0))
-            if skip == 0 and n < all_[b]:  # where the join looks for the sequence's pieces
-                count = 2 + (all_[b] - n - 1) // each
-                assert (begin[b + 1] - 1) // each - x + 1 == count
+            done, own = max(skip - PIECE, 0), all_[b] - PIECE
+            mine = skip + n - PIECE - done  # tiles of its own in this piece
+            if mine > 0:
+                seen[b] += mine
+                if mine < own:
+                    places.append(2 * x + (done == 0))
+                if done == 0 and mine < own:  # where the join looks for the sequence's pieces
+                    count = 2 + (own - mine - 1) // each
+                    assert (begin[b + 1] - 1) // each - x + 1 == count
             tiles, b, skip = tiles - n, b + 1, 0
+    assert seen == [t - PIECE for t in all_]
     assert len(set(places)) == len(places) and max(places, default=0) < 2 * runs
 
 
