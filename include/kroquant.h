@@ -458,21 +458,27 @@ kq_status kq_paged_attention(const void* q, kq_dtype dtype, int64_t B, int64_t q
                              const int32_t* lengths, float scale, int64_t window, void* out, int64_t out_seq,
                              int64_t out_head, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Bytes of device workspace that kq_w4a16_linear uses for these sizes (0: none). */
+kq_status kq_w4a16_workspace_size(int64_t M, int64_t N, int64_t K, kq_dtype x_dtype, size_t* bytes);
+
 /*
  * kq_w4a16_linear -- kq_mxfp4_linear for a few rows whose activations are not
  * quantized (a decoding loop's):
  *     out = residual + gate act(x deq(B)^T + bias)
- *   x        [M, K] of x_dtype, row stride ldx >= K elements
- *   others   as for kq_mxfp4_linear
+ *   x          [M, K] of x_dtype, row stride ldx >= K elements
+ *   workspace  device, 16-byte aligned, kq_w4a16_workspace_size bytes, scratch between
+ *              calls; or NULL, which is slower where that size is not 0
+ *   others     as for kq_mxfp4_linear
  * The weight is read once for each 16 rows.  Products of bf16 values are exact, x in
  * 32 bits takes part in full (finite values only); sums are in 32 bits, in a fixed
- * order.  M is at most 65535 * 16.  M, N = 0 is a no-op.  Enqueued on `stream`; no
- * allocation, no synchronization.
+ * order for given sizes.  M is at most 65535 * 16.  M, N = 0 is a no-op.  Enqueued on
+ * `stream`; no allocation, no synchronization.
  */
 kq_status kq_w4a16_linear(const void* x, kq_dtype x_dtype, int64_t M, int64_t ldx, const uint8_t* b_codes,
                           const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
                           int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act, const void* residual,
-                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream);
+                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /*
  * kq_mxfp4_quantize -- the bare MXFP4 quantizer ("Q4", the lower bound of

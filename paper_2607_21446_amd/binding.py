@@ -43,7 +43,7 @@ EXPORTED = (
     "kq_mxfp4_linear", "kq_mxfp4_grouped_linear", "kq_block_norm", "kq_block_norm_workspace_size",
     "kq_block_norm_backward",
     "kq_rope", "kq_kv_cache_write", "kq_kv_cache_read", "kq_paged_attention_workspace_size", "kq_paged_attention",
-    "kq_w4a16_linear",
+    "kq_w4a16_workspace_size", "kq_w4a16_linear",
     "kq_status_string", "kq_last_error_detail", "kq_version",
 )
 
@@ -105,7 +105,8 @@ def lib() -> ctypes.CDLL:
     L.kq_kv_cache_read.argtypes = [C, P, I64, P, P, I, P]
     L.kq_paged_attention_workspace_size.argtypes = [I64, I64, I64, I64, ctypes.POINTER(ctypes.c_size_t)]
     L.kq_paged_attention.argtypes = [P, I, I64, I64, I64, I64, C, P, I64, I64, P, F, I64, P, I64, I64, P, P, ctypes.c_size_t, P]
-    L.kq_w4a16_linear.argtypes = [P, I, I64, I64, P, P, I64, I64, P, P, I64, I64, I, I, P, I64, P, I64, I, P]
+    L.kq_w4a16_workspace_size.argtypes = [I64, I64, I64, I, ctypes.POINTER(ctypes.c_size_t)]
+    L.kq_w4a16_linear.argtypes = [P, I, I64, I64, P, P, I64, I64, P, P, I64, I64, I, I, P, I64, P, I64, I, P, ctypes.c_size_t, P]
     for name in EXPORTED[:-3]:
         getattr(L, name).restype = ctypes.c_int
     L.kq_status_string.argtypes = [I]
@@ -906,13 +907,22 @@ def paged_attention(q, cache, page_table, lengths, scale=None, window=None, out=
     return out if lse is None else (out, lse)
 
 
-def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=None, out=None, out_dtype=None, stream=None):
+def w4a16_workspace(M, N, K, x_dtype=torch.bfloat16, device="cuda"):
+    """Device workspace of w4a16_linear for these sizes (it may be of no bytes)."""
+    n = ctypes.c_size_t(0)
+    _check(lib().kq_w4a16_workspace_size(M, N, K, _FLOATS[x_dtype], ctypes.byref(n)), "kq_w4a16_workspace_size")
+    return torch.empty(int(n.value), dtype=torch.uint8, device=device)
+
+
+def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=None, out=None, out_dtype=None, workspace=None,
+                 stream=None):
     """kq_w4a16_linear: out = residual + gate * act(x deq(B)^T + bias) for a few rows x
     [M, K] of fp32 or bf16 that are not quantized (a decoding loop's) and an MXFP4
     weight b_codes [N, K/2], b_scales [N, K/32].  The other arguments are
-    mxfp4_linear's.  Returns out."""
+    mxfp4_linear's; a ``workspace`` of w4a16_workspace is made if it is not given (two
+    calls that may run at once need one each).  Returns out."""
     a = _one_of(_ACTS, act, "act")
-    r = _native().w4a16_linear(x, b_codes, b_scales, bias, a, gate, residual, out, out_dtype, stream)
+    r = _native().w4a16_linear(x, b_codes, b_scales, bias, a, gate, residual, out, out_dtype, workspace, stream)
     if r is not None:
         return r
     for t, name in ((b_codes, "b_codes"), (b_scales, "b_scales")):
@@ -938,11 +948,18 @@ def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=
         out_dtype = residual.dtype
     out, ldo = _linear_out(out, M, cols, out_dtype, dev)
     ldr = 0 if residual is None else _rows_of(residual, (M, cols), "residual", dev, out.dtype)
+    if workspace is None:
+        with torch.cuda.device(dev), _scratch_of(stream, dev):
+            workspace = w4a16_workspace(M, N, K, x.dtype, dev)
+    _need(workspace, torch.uint8, "workspace")
+    if workspace.device != dev:
+        raise ValueError(f"workspace is on {workspace.device}, x on {dev}")
     guard, st = _at(dev, stream)
     with guard:
         _check(lib().kq_w4a16_linear(_ptr(x), _FLOATS[x.dtype], M, ldx, _ptr(b_codes), _ptr(b_scales), N, K, _ptr(bias), _ptr(gate),
                                      strides[0], max(1, M // B), vec if gate is None else gvec, a, _ptr(residual), ldr, _ptr(out), ldo,
-                                     _FLOATS[out.dtype], st), "kq_w4a16_linear")
+                                     _FLOATS[out.dtype], _ptr(workspace) if workspace.numel() else None, workspace.numel(), st),
+               "kq_w4a16_linear")
     return out
 
 

@@ -790,10 +790,20 @@ kq_status kq_paged_attention(const void* q, kq_dtype dtype, int64_t B, int64_t q
     return from_hip(kq::launch_attn(p, (hipStream_t)stream), "kq_paged_attention");
 }
 
+kq_status kq_w4a16_workspace_size(int64_t M, int64_t N, int64_t K, kq_dtype x_dtype, size_t* bytes) {
+    if (!dtype_ok(x_dtype)) return fail(KQ_ERROR_INVALID_VALUE, "x_dtype = %d must be a kq_dtype", (int)x_dtype);
+    const kq_status st = check_linear(nullptr, nullptr, M, nullptr, nullptr, N, K, nullptr, 0, 0, nullptr, N, 0);
+    if (st != KQ_SUCCESS && st != KQ_ERROR_NULL_POINTER) return st;
+    if (!bytes) return fail(KQ_ERROR_NULL_POINTER, "bytes must not be NULL");
+    *bytes = M > 0 && N > 0 ? (size_t)kq::matvec_workspace(M, N, K, x_dtype == KQ_DTYPE_BF16) : 0;
+    return ok();
+}
+
 kq_status kq_w4a16_linear(const void* x, kq_dtype x_dtype, int64_t M, int64_t ldx, const uint8_t* b_codes,
                           const uint8_t* b_scales, int64_t N, int64_t K, const void* bias, const void* gate,
                           int64_t gate_stride, int64_t gate_rows, kq_dtype vec_dtype, kq_act act, const void* residual,
-                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* stream) {
+                          int64_t ldr, void* out, int64_t ldo, kq_dtype out_dtype, void* workspace, size_t workspace_bytes,
+                          void* stream) {
     if (!dtype_ok(x_dtype)) return fail(KQ_ERROR_INVALID_VALUE, "x_dtype = %d must be a kq_dtype", (int)x_dtype);
     // (the weight stands in for the operand that this call does not have)
     const kq_status st = check_linear(b_codes, b_scales, M, b_codes, b_scales, N, K, bias, vec_dtype, act, out, ldo, out_dtype);
@@ -809,7 +819,12 @@ kq_status kq_w4a16_linear(const void* x, kq_dtype x_dtype, int64_t M, int64_t ld
     if (M == 0 || N == 0) return ok();
     if (!x) return fail(KQ_ERROR_NULL_POINTER, "x must not be NULL");
     if (!aligned(x, dtype_bytes(x_dtype))) return fail(KQ_ERROR_MISALIGNED, "x must be aligned to its elements");
+    if (!aligned(workspace, 16)) return fail(KQ_ERROR_MISALIGNED, "workspace must be 16-byte aligned");
+    const int64_t need = kq::matvec_workspace(M, N, K, x_dtype == KQ_DTYPE_BF16);
+    if (workspace && workspace_bytes < (size_t)need)
+        return fail(KQ_ERROR_INVALID_VALUE, "workspace holds %zu bytes, the call needs %lld", workspace_bytes, (long long)need);
     kq::MatvecParams p{};
+    p.partial = need > 0 ? static_cast<float*>(workspace) : nullptr;
     p.x = x;
     p.ldx = ldx;
     p.x16 = x_dtype == KQ_DTYPE_BF16;

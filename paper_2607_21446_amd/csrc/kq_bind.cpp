@@ -906,15 +906,15 @@ PyObject* paged_attention(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
-// (x, b_codes, b_scales, bias, act, gate, residual, out, out_dtype, stream)
+// (x, b_codes, b_scales, bias, act, gate, residual, out, out_dtype, workspace, stream)
 PyObject* w4a16_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    if (n != 10) Py_RETURN_NONE;
+    if (n != 11) Py_RETURN_NONE;
     return guarded([&]() -> PyObject* {
         const at::Tensor *x = tensor(v[0]), *b = tensor(v[1]), *s = tensor(v[2]);
         int act, xt;
         void* st = nullptr;
         if (!x || !x->is_cuda() || x->dim() != 2 || !float_type(x, &xt) || !matrix(b, at::kByte) || !matrix(s, at::kByte) ||
-            !small_int(v[4], &act) || !stream_of(v[9], &st))
+            !small_int(v[4], &act) || !stream_of(v[10], &st))
             return nullptr;
         const at::Device dev = x->device();
         const int64_t M = x->size(0), K = x->size(1), N = b->size(0);
@@ -939,12 +939,27 @@ PyObject* w4a16_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
         int64_t ldo, ldr = 0;
         if (!linear_out(v[7], v[8], type, M, cols, dev, out, &ldo, &type)) return nullptr;
         if (res && (ldr = row_stride(res, M, cols, type, dev)) < 0) return nullptr;
+        size_t bytes = 0;
+        at::Tensor made;
+        void* work = nullptr;
+        if (v[9] != Py_None) {
+            const at::Tensor* w = tensor(v[9]);
+            if (!dense(w, at::kByte) || w->device() != dev) return nullptr;
+            bytes = w->numel();
+            work = bytes ? w->data_ptr() : nullptr;
+        } else {  // (one of the current stream's; for another stream Python makes it)
+            if (kq_w4a16_workspace_size(M, N, K, (kq_dtype)xt, &bytes) != KQ_SUCCESS || (bytes && v[10] != Py_None)) return nullptr;
+            if (bytes) {
+                made = empty({(int64_t)bytes}, at::kByte, dev);
+                work = made.data_ptr();
+            }
+        }
         if (!call("kq_w4a16_linear", [&] {
                 return kq_w4a16_linear(x->data_ptr(), (kq_dtype)xt, M, ldx, static_cast<const uint8_t*>(b->data_ptr()),
                                        static_cast<const uint8_t*>(s->data_ptr()), N, K, bias, gate, stride,
                                        std::max<int64_t>(1, M / vec.count()), (kq_dtype)vec.dtype(), (kq_act)act,
                                        res ? res->data_ptr() : nullptr, ldr, out.ptr, ldo,
-                                       type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, st);
+                                       type == at::kBFloat16 ? KQ_DTYPE_BF16 : KQ_DTYPE_FP32, work, bytes, st);
             }))
             return nullptr;
         return out.take();

@@ -95,7 +95,10 @@ struct MatvecParams {
     int64_t ldx;
     int x16;  // 1: bf16, 0: fp32
     LinearParams l;  // weight, sizes, epilogue; no A
+    float* partial;  // matvec_workspace bytes, or null: a form without
+    int64_t columns;  // of its rows, filled in by the launcher
 };
-hipError_t launch_matvec(const MatvecParams& p, hipStream_t st);
+int64_t matvec_workspace(int64_t M, int64_t N, int64_t K, bool x16);  // 0: none is used
+hipError_t launch_matvec(MatvecParams p, hipStream_t st);
 
 }  // namespace kq

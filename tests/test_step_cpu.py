@@ -134,7 +134,7 @@ def test_attention_workspace_size():
 
 def _w4a16(**kw):
     a = dict(x=FAKE, xt=1, M=4, ldx=64, bc=FAKE, bs=FAKE, N=6, K=64, bias=None, gate=None, gs=0, gr=4, vt=0, act=0, res=None, ldr=0,
-             out=FAKE, ldo=6, ot=1)
+             out=FAKE, ldo=6, ot=1, ws=None, wsb=0)
     assert set(kw) <= set(a)
     return kq.lib().kq_w4a16_linear(*{**a, **kw}.values(), None)
 
@@ -146,11 +146,23 @@ def _w4a16(**kw):
     (dict(ldx=63), INVALID), (dict(gate=FAKE, gr=0), INVALID), (dict(gate=FAKE, gs=-1), INVALID), (dict(res=FAKE, ldr=5), INVALID),
     (dict(x=None), NULLP), (dict(bc=None), NULLP), (dict(bs=None), NULLP), (dict(out=None), NULLP), (dict(bc=FAKE + 8), MISALIGNED),
     (dict(x=FAKE + 1), MISALIGNED), (dict(xt=0, x=FAKE + 2), MISALIGNED), (dict(out=FAKE + 1), MISALIGNED), (dict(bias=FAKE + 2), MISALIGNED),
-    (dict(gate=FAKE + 2), MISALIGNED), (dict(res=FAKE + 1, ldr=6), MISALIGNED), (dict(M=0), SUCCESS), (dict(N=0, ldo=0), SUCCESS),
+    (dict(gate=FAKE + 2), MISALIGNED), (dict(res=FAKE + 1, ldr=6), MISALIGNED), (dict(ws=FAKE + 8), MISALIGNED),
+    (dict(M=16, K=12288, ldx=12288, ws=FAKE, wsb=8), INVALID), (dict(M=0), SUCCESS), (dict(N=0, ldo=0), SUCCESS),
     (dict(M=0, x=None, out=None), SUCCESS),
 ])
 def test_w4a16_rejects(kw, status):
     assert _w4a16(**kw) == status and _said(status)
+
+
+def test_w4a16_workspace_size():
+    n = ctypes.c_size_t(0)
+    ws = lambda M, N, K, t: kq.lib().kq_w4a16_workspace_size(M, N, K, t, ctypes.byref(n))  # noqa: E731
+    assert ws(-1, 8, 64, 1) == INVALID and ws(1, 8, 40, 1) == INVALID and ws(1, 8, 64, 2) == INVALID
+    assert kq.lib().kq_w4a16_workspace_size(1, 8, 64, 1, None) == NULLP
+    for M, N, K, t, used in ((0, 8, 64, 1, False), (1, 4096, 4096, 1, False), (16, 4096, 2240, 0, False), (17, 4096, 12288, 0, False),
+                             (16, 4097, 12288, 0, True), (16, 4096, 12288, 1, True), (1, 1, 1 << 20, 1, True)):
+        assert ws(M, N, K, t) == SUCCESS and (n.value > 0) == used, (M, N, K, t)
+        assert not used or n.value >= 4 * M * N * (K // 512)
 
 
 def test_binding_names_what_is_wrong():
