@@ -38,7 +38,7 @@ typedef uint32_t u32x4e __attribute__((ext_vector_type(4), aligned(2)));  // at 
 constexpr int kVecRows = 16;   // of a workgroup, of the weight and of x
 constexpr int kVecWaves = 8;   // of a workgroup
 constexpr int kRunBlocks = 16;  // of a wave's run of columns
-constexpr int kResidentBytes = 100 << 10;
+constexpr int kResidentBytes = 136 << 10;
 constexpr int kResidentColumns = 4096;  // from here on: below, a run leaves most waves without one
 
 template <int I, int N, class Fn>
@@ -281,7 +281,8 @@ __device__ __forceinline__ void stage_rows(uint8_t* xs, int stride, const uint8_
     }
 }
 
-// A run's products: lane (r, g)'s blocks 4 g .. 4 g + 3 of the weight, those before `left` existing, with x's at `from`.
+// A run's products in two sums: lane (r, g)'s blocks 4 g .. 4 g + 3 of the weight, those before `left` existing, with x's
+// at `from`.
 template <bool X16>
 __device__ __forceinline__ void add_run(f32x4 (&acc)[2], const Weights& w, const uint8_t* from, int left) {
     unrolled<0, 4>([&](auto sub) KQ_INLINE {
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecP
     const int blocks = (int)(l.g.K / 32), rows = (int)l.g.M, stride = lds_stride<X16>(blocks);
     const WeightRows at(l.g, n0);
     constexpr int kStep = kRunBlocks * kVecWaves;
-    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 acc[2] = {};
     Weights w, next;
     int b0 = kRunBlocks * wave;
     if (b0 < blocks) next.load(at.codes, at.scales, b0, blocks);
@@ -349,11 +350,11 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecP
         w.settle();
         add_run<X16>(acc, w, mine + b0 * (kTerms<X16> * 64), blocks - b0);
     }
-    acc[0] += acc[1];
-    finish_tile(l, 0, n0, acc[0]);
+    finish_tile(l, 0, n0, acc[0] + acc[1]);
 }
 
-// Slice blockIdx.y of the columns, for every gridDim.x-th eight tiles of the weight: a wave a tile.
+// Slice blockIdx.y of the columns, for every gridDim.x-th eight tiles of the weight: a wave a tile.  (Two tiles a wave, which
+// share x's reads from LDS, leave two waves a SIMD and took 18 us for 16.)
 template <bool X16>
 __global__ __launch_bounds__(64 * kVecWaves) void matvec_slice_kernel(MatvecParams p) {
     extern __shared__ uint8_t xs[];
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_slice_kernel(MatvecPara
             next.load(at.codes, at.scales, b0, blocks);
         }
         w.settle();
-        f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        f32x4 acc[2] = {};
         add_run<X16>(acc, w, from, mine);
         if (r < rows) *reinterpret_cast<f32x4*>(out + n0) = acc[0] + acc[1];
     }
@@ -425,8 +426,8 @@ hipError_t launch_matvec(MatvecParams p, hipStream_t st) {
         if (p.x16) matvec_resident_kernel<true><<<grid, 64 * kVecWaves, resident, st>>>(p);
         else matvec_resident_kernel<false><<<grid, 64 * kVecWaves, resident, st>>>(p);
     } else if (p.partial) {
-        const int64_t slices = vec_slices(K), eights = (tiles + kVecWaves - 1) / kVecWaves;
         p.columns = vec_columns(N);
+        const int64_t slices = vec_slices(K), eights = (tiles + kVecWaves - 1) / kVecWaves;
         // as many workgroups as the GPU holds, each with the same number of tiles a wave
         const int64_t turns = std::max<int64_t>(1, (eights * slices + 767) / 768);
         const dim3 shares((unsigned)((eights + turns - 1) / turns), (unsigned)slices);
