@@ -689,7 +689,9 @@ def _check_linear(M, N, K, x=BF16, act=None, bias=True, B=0, residual=False, out
 
 # rows on either side of a tile of 16, ragged widths, K of a block, of parts of a step, of many
 W4A16 = [(1, 1, 32), (1, 2, 64), (1, 17, 96), (2, 130, 2016), (1, 3000, 512), (3, 16, 128), (15, 64, 288), (16, 48, 256), (17, 100, 1152),
-         (32, 33, 160), (33, 514, 480), (50, 1000, 4096), (1, 4096, 12288), (8, 11200, 2240), (5, 66, 16384), (130, 200, 320)]
+         (32, 33, 160), (33, 514, 480), (50, 1000, 4096), (1, 4096, 12288), (8, 11200, 2240), (5, 66, 16384), (130, 200, 320),
+         # x's rows in LDS, and slices of the columns: runs of 512 and what is left of them, few and many tiles a wave
+         (1, 33, 4128), (3, 70, 4096), (16, 330, 4096), (7, 50, 4576), (16, 100, 8224), (2, 18, 12320), (16, 2600, 6400), (11, 1, 5120)]
 
 
 @pytest.mark.parametrize("M,N,K", W4A16)
@@ -711,6 +713,23 @@ def test_w4a16_epilogues(M, N, K, act, out):
         _check_linear(M, N, K, x, act=act, bias=False, B=1, residual=True, out=out, strided=True)
         for B in [b for b in (2, 3, M) if M % b == 0]:  # batches that end inside a tile, and one for each row
             _check_linear(M, N, K, x, act=act, bias=True, B=B, residual=B == 2, out=out, vec=BF16)
+
+
+@pytest.mark.parametrize("M,N,K,x", [(16, 200, 8192, BF16), (9, 130, 4160, FP32), (1, 70, 100000, FP32)])
+def test_w4a16_workspaces(M, N, K, x):
+    """Given and dirty, of the call's own, and none: the form without one has sums of another order."""
+    g = _gen(36)
+    xv, w = _randn(g, M, K, dtype=x), _codes(g, N, K)
+    ws = kq.w4a16_workspace(M, N, K, x)
+    assert ws.numel() >= 4 * M * N * (K // 512)
+    want, err = _linear64(xv, _weight64(*w), None, None, None, None)
+    got = kq.w4a16_linear(xv, *w, out_dtype=FP32)
+    _within(got, want, err + _stored(want, FP32), "own")
+    for fill in (0, 255):
+        assert torch.equal(kq.w4a16_linear(xv, *w, out_dtype=FP32, workspace=ws.fill_(fill)), got)
+    _within(kq.w4a16_linear(xv, *w, out_dtype=FP32, workspace=ws[:0]), want, err + _stored(want, FP32), "none")
+    with pytest.raises(kq.KQError):
+        kq.w4a16_linear(xv, *w, workspace=ws[:-16])
 
 
 def test_w4a16_of_wide_ranges():
