@@ -9,11 +9,11 @@
 // bits: exact).
 //
 // Bound by the weight's read.  Three forms, by what x takes:
-//   narrow    K below 4096: a workgroup's waves take the columns of 16 rows in
+//   narrow    K below 2048: a workgroup's waves take the columns of 16 rows in
 //             turn, x as the operands need it; also whatever fits no other form;
 //   resident  all of x's rows (16 at most) fit in LDS: as above with x in LDS,
-//             as terms, and the weight in runs of 512 columns;
-//   slices    they do not: workgroups take a run's columns for many rows of the
+//             as terms, and the weight's loads 64 bytes a row;
+//   slices    they do not: workgroups take 512 columns of many rows of the
 //             weight, x's slice in LDS, and a second launch adds the slices' sums.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -37,9 +37,11 @@ typedef uint32_t u32x4e __attribute__((ext_vector_type(4), aligned(2)));  // at 
 
 constexpr int kVecRows = 16;   // of a workgroup, of the weight and of x
 constexpr int kVecWaves = 8;   // of a workgroup
-constexpr int kRunBlocks = 16;  // of a wave's run of columns
+constexpr int kStepBlocks = 4;    // of a wave's step: 128 columns
+constexpr int kSliceBlocks = 16;  // of a slice: 512 columns
+constexpr int kAhead = 2;           // steps that a wave has loaded or is loading
 constexpr int kResidentBytes = 136 << 10;
-constexpr int kResidentColumns = 4096;  // from here on: below, a run leaves most waves without one
+constexpr int kResidentColumns = 2048;  // from here on: one row through 1152 x 1152 took 3.1 us for 2.7
 
 template <int I, int N, class Fn>
 __device__ __forceinline__ void unrolled(Fn f) {
@@ -202,7 +204,120 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_narrow_kernel(MatvecPar
     finish_tile(l, m0, n0, acc);
 }
 
-// ------------------------------------------------------------ runs of 512 columns
+// ------------------------------------------------------------ x in LDS
+
+// A step of a wave: four blocks of 16 of the weight's rows.  Four neighbouring lanes read a row's 64 bytes, and an exchange
+// gives lane (r, g) its own row's block g.  (A row a lane, as the operand needs it, costs the cache an access for every lane:
+// 16 bf16 rows and a weight of 12288 x 12288 took 49 us so.)
+struct Step {
+    u32x4v w;
+    uint32_t s;
+    // codes, scales: of the row lane / 4; b0: the first block.  Blocks past the last are read as the last (and dropped later).
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int b0, int blocks) {
+        const int b = min(b0 + (int)(threadIdx.x & 3), blocks - 1);
+        w = *reinterpret_cast<const u32x4v*>(codes + 16 * (int64_t)b);
+        s = scales[b];
+    }
+    __device__ __forceinline__ void settle() {
+        const int from = (16 * (int)(threadIdx.x & 15) + 4 * ((int)(threadIdx.x & 63) >> 4));  // four times the lane
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)w[i]);
+        s = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)s);
+    }
+};
+
+// x's rows in LDS as terms: row r's block b of `blocks` from r stride + b terms 64 on, a block's terms one after another.
+// Rows are 16 bytes more than a multiple of 128 apart, so that eight lanes' rows lie in different banks.
+template <bool X16>
+__device__ __forceinline__ int lds_stride(int blocks) {
+    return blocks * kTerms<X16> * 64 + 16 + (blocks * kTerms<X16> & 1) * 64;
+}
+// Blocks b0 .. b0 + blocks - 1 of `rows` rows.
+template <bool X16>
+__device__ __forceinline__ void stage_rows(uint8_t* xs, int stride, const uint8_t* x, int64_t row_bytes, int rows, int b0, int blocks) {
+    const int each = 4 * blocks, all = rows * each;  // eights of values
+    constexpr int kBytes = X16 ? 16 : 32, kAtOnce = X16 ? 4 : 2;
+    for (int i = threadIdx.x; i < all; i += kAtOnce * 64 * kVecWaves) {
+        u32x4v t[kAtOnce][kTerms<X16>];
+        int to[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int at = min(i + j * 64 * kVecWaves, all - 1), row = at / each, e = at - row * each;
+            load_terms<X16>(x + row * row_bytes + ((int64_t)b0 * 4 + e) * kBytes, t[j]);
+            to[j] = row * stride + (e >> 2) * (kTerms<X16> * 64) + (e & 3) * 16;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+            for (int n = 0; n < kTerms<X16>; ++n) *reinterpret_cast<u32x4v*>(xs + to[j] + 64 * n) = t[j][n];
+    }
+}
+
+// A step's products in two sums: lane (r, g)'s block g of the weight, of which `left` exist, with x's at `from`.
+template <bool X16>
+__device__ __forceinline__ void add_step(f32x4 (&acc)[2], Step& w, const uint8_t* from, int left) {
+    u32x4v t[4][kTerms<X16>];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int n = 0; n < kTerms<X16>; ++n) t[k][n] = *reinterpret_cast<const u32x4v*>(from + n * 64 + 16 * k);
+    w.settle();
+    if (left < kStepBlocks) {
+        asm volatile("");  // a branch: the last step only
+        const bool in = (int)((threadIdx.x & 63) >> 4) < left;
+        w.s = in ? w.s : 127u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w.w[k] = in ? w.w[k] : 0u;
+#pragma unroll
+            for (int n = 0; n < kTerms<X16>; ++n) t[k][n] = in ? t[k][n] : u32x4v{0u, 0u, 0u, 0u};
+        }
+    }
+    const float sc = mx_scale(w.s);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bf16x8 a = weight_operand(w.w[k], sc);
+#pragma unroll
+        for (int n = 0; n < kTerms<X16>; ++n)
+            acc[k & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, t[k][n]), acc[k & 1], 0, 0, 0);
+    }
+}
+
+template <bool X16>
+__global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecParams p) {
+    extern __shared__ uint8_t xs[];
+    const LinearParams& l = p.l;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * kVecRows, row = min(n0 + (lane >> 2), l.g.N - 1);
+    const int blocks = (int)(l.g.K / 32), rows = (int)l.g.M, stride = lds_stride<X16>(blocks);
+    const uint8_t* const codes = l.g.b_codes + row * (l.g.K / 2);
+    const uint8_t* const scales = l.g.b_scales + row * blocks;
+    constexpr int kStep = kStepBlocks * kVecWaves;
+    f32x4 acc[2] = {};
+    Step w[kAhead];
+    int b0 = kStepBlocks * wave;
+    unrolled<0, kAhead - 1>([&](auto stage) KQ_INLINE {
+        if (b0 + stage * kStep < blocks) w[stage].load(codes, scales, b0 + stage * kStep, blocks);
+    });
+    stage_rows<X16>(xs, stride, static_cast<const uint8_t*>(p.x), p.ldx * (X16 ? 2 : 4), rows, 0, blocks);
+    __syncthreads();
+    const uint8_t* const mine = xs + min(r, rows - 1) * stride + g * (kTerms<X16> * 64);
+    while (b0 < blocks) {
+        bool more = true;
+        unrolled<0, kAhead>([&](auto stage) KQ_INLINE {
+            constexpr int now = stage, late = (stage + kAhead - 1) % kAhead;
+            if (!more) return;
+            const int at = b0 + (kAhead - 1) * kStep;
+            if (at < blocks) w[late].load(codes, scales, at, blocks);
+            add_step<X16>(acc, w[now], mine + b0 * (kTerms<X16> * 64), blocks - b0);
+            b0 += kStep;
+            more = b0 < blocks;
+        });
+    }
+    finish_tile(l, 0, n0, acc[0] + acc[1]);
+}
+
+// ------------------------------------------------------------ slices
 
 // Word i of lane q of every four lanes becomes word q of lane i.
 __device__ __forceinline__ void quad_transpose(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
@@ -219,11 +334,11 @@ __device__ __forceinline__ void quad_transpose(uint32_t& a, uint32_t& b, uint32_
     d = high ? d1 : gb;
 }
 
-// Four neighbouring lanes read 64 bytes of one of the weight's rows: lane 4 i + q the block q + 4 (i / 4) of row
-// 4 (i % 4) + k in load k; the transpose of the four loads then gives lane (r, g) its own row's blocks 4 g .. 4 g + 3.
-// (A row a lane, as the operand needs it, costs the cache an access for every lane: 16 bf16 rows and a weight of 12288 x
-// 12288 took 49 us so.)
-struct Weights {
+// A slice of 16 of the weight's rows: 16 blocks, four side by side a lane.  Loads as for a step, 64 bytes of a row by four
+// neighbouring lanes: lane 4 i + q reads the block q + 4 (i / 4) of row 4 (i % 4) + k in load k, and the transpose of the four
+// loads gives lane (r, g) its own row's blocks 4 g .. 4 g + 3.  (LDS is what this form waits for, x's 48 KB a tile in 32 bits:
+// with a step's exchange it took 16.7 us, with this one 15.8.)
+struct Run {
     u32x4v w[4];  // after `settle`: block 4 g + k of row r
     uint32_t s;   // their scales
     // b0: the first block of 16, of which those before `blocks` exist; others are read as the last (and dropped later)
@@ -254,37 +369,10 @@ struct Weights {
 };
 
 
-// x's rows in LDS as terms: row r's block b of `blocks` from r stride + b terms 64 on, a block's terms one after another.
-// Rows are 16 bytes more than a multiple of 128 apart, so that eight lanes' rows lie in different banks.
-template <bool X16>
-__device__ __forceinline__ int lds_stride(int blocks) {
-    return blocks * kTerms<X16> * 64 + 16 + (blocks * kTerms<X16> & 1) * 64;
-}
-// Blocks b0 .. b0 + blocks - 1 of `rows` rows.
-template <bool X16>
-__device__ __forceinline__ void stage_rows(uint8_t* xs, int stride, const uint8_t* x, int64_t row_bytes, int rows, int b0, int blocks) {
-    const int each = 4 * blocks, all = rows * each;  // eights of values
-    constexpr int kBytes = X16 ? 16 : 32, kAtOnce = X16 ? 4 : 2;
-    for (int i = threadIdx.x; i < all; i += kAtOnce * 64 * kVecWaves) {
-        u32x4v t[kAtOnce][kTerms<X16>];
-        int to[kAtOnce];
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int at = min(i + j * 64 * kVecWaves, all - 1), row = at / each, e = at - row * each;
-            load_terms<X16>(x + row * row_bytes + ((int64_t)b0 * 4 + e) * kBytes, t[j]);
-            to[j] = row * stride + (e >> 2) * (kTerms<X16> * 64) + (e & 3) * 16;
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-#pragma unroll
-            for (int n = 0; n < kTerms<X16>; ++n) *reinterpret_cast<u32x4v*>(xs + to[j] + 64 * n) = t[j][n];
-    }
-}
-
 // A run's products in two sums: lane (r, g)'s blocks 4 g .. 4 g + 3 of the weight, those before `left` existing, with x's
 // at `from`.
 template <bool X16>
-__device__ __forceinline__ void add_run(f32x4 (&acc)[2], const Weights& w, const uint8_t* from, int left) {
+__device__ __forceinline__ void add_run(f32x4 (&acc)[2], const Run& w, const uint8_t* from, int left) {
     unrolled<0, 4>([&](auto sub) KQ_INLINE {
         constexpr int S = sub;
         uint32_t c[4], s = w.s >> (8 * S) & 255u;
@@ -295,7 +383,7 @@ __device__ __forceinline__ void add_run(f32x4 (&acc)[2], const Weights& w, const
 #pragma unroll
             for (int n = 0; n < kTerms<X16>; ++n) t[k][n] = *reinterpret_cast<const u32x4v*>(from + (S * kTerms<X16> + n) * 64 + 16 * k);
         }
-        if (left < kRunBlocks) {
+        if (left < kSliceBlocks) {
             asm volatile("");  // a branch: the last run only
             const bool in = 4 * (int)((threadIdx.x & 63) >> 4) + S < left;
             s = in ? s : 127u;
@@ -328,31 +416,6 @@ struct WeightRows {
     }
 };
 
-template <bool X16>
-__global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecParams p) {
-    extern __shared__ uint8_t xs[];
-    const LinearParams& l = p.l;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * kVecRows;
-    const int blocks = (int)(l.g.K / 32), rows = (int)l.g.M, stride = lds_stride<X16>(blocks);
-    const WeightRows at(l.g, n0);
-    constexpr int kStep = kRunBlocks * kVecWaves;
-    f32x4 acc[2] = {};
-    Weights w, next;
-    int b0 = kRunBlocks * wave;
-    if (b0 < blocks) next.load(at.codes, at.scales, b0, blocks);
-    stage_rows<X16>(xs, stride, static_cast<const uint8_t*>(p.x), p.ldx * (X16 ? 2 : 4), rows, 0, blocks);
-    __syncthreads();
-    const uint8_t* const mine = xs + min(r, rows - 1) * stride + 4 * g * (kTerms<X16> * 64);
-    for (; b0 < blocks; b0 += kStep) {
-        w = next;
-        if (b0 + kStep < blocks) next.load(at.codes, at.scales, b0 + kStep, blocks);
-        w.settle();
-        add_run<X16>(acc, w, mine + b0 * (kTerms<X16> * 64), blocks - b0);
-    }
-    finish_tile(l, 0, n0, acc[0] + acc[1]);
-}
-
 // Slice blockIdx.y of the columns, for every gridDim.x-th eight tiles of the weight: a wave a tile.  (Two tiles a wave, which
 // share x's reads from LDS, leave two waves a SIMD and took 18 us for 16.)
 template <bool X16>
@@ -360,11 +423,11 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_slice_kernel(MatvecPara
     extern __shared__ uint8_t xs[];
     const LinearParams& l = p.l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int blocks = (int)(l.g.K / 32), rows = (int)l.g.M, b0 = kRunBlocks * blockIdx.y, mine = min(blocks - b0, kRunBlocks);
-    constexpr int kStride = kRunBlocks * kTerms<X16> * 64 + 16;
+    const int blocks = (int)(l.g.K / 32), rows = (int)l.g.M, b0 = kSliceBlocks * blockIdx.y, mine = min(blocks - b0, kSliceBlocks);
+    constexpr int kStride = kSliceBlocks * kTerms<X16> * 64 + 16;
     const int64_t step = (int64_t)gridDim.x * kVecWaves * kVecRows;
     int64_t n0 = ((int64_t)blockIdx.x * kVecWaves + wave) * kVecRows;
-    Weights w, next;
+    Run w, next;
     if (n0 < l.g.N) {
         const WeightRows at(l.g, n0);
         next.load(at.codes, at.scales, b0, blocks);
@@ -404,7 +467,7 @@ __global__ __launch_bounds__(256) void matvec_sum_kernel(MatvecParams p, int sli
     });
 }
 
-int64_t vec_slices(int64_t K) { return (K / 32 + kRunBlocks - 1) / kRunBlocks; }
+int64_t vec_slices(int64_t K) { return (K / 32 + kSliceBlocks - 1) / kSliceBlocks; }
 int64_t vec_columns(int64_t N) { return (N + kVecRows - 1) / kVecRows * kVecRows; }
 
 // Bytes of x's rows in LDS.
@@ -414,7 +477,7 @@ int64_t resident_bytes(int64_t M, int64_t K, bool x16) { return M * (K / 32 * (x
 
 // Only the slices' form has one.
 int64_t matvec_workspace(int64_t M, int64_t N, int64_t K, bool x16) {
-    if (M > kVecRows || K < kResidentColumns || resident_bytes(M, K, x16) <= kResidentBytes) return 0;
+    if (M > kVecRows || K < kResidentColumns || vec_slices(K) > 65535 || resident_bytes(M, K, x16) <= kResidentBytes) return 0;
     return vec_slices(K) * M * vec_columns(N) * (int64_t)sizeof(float);
 }
 
@@ -431,7 +494,7 @@ hipError_t launch_matvec(MatvecParams p, hipStream_t st) {
         // as many workgroups as the GPU holds, each with the same number of tiles a wave
         const int64_t turns = std::max<int64_t>(1, (eights * slices + 767) / 768);
         const dim3 shares((unsigned)((eights + turns - 1) / turns), (unsigned)slices);
-        const size_t lds = resident_bytes(M, 32 * kRunBlocks, p.x16);
+        const size_t lds = resident_bytes(M, 32 * kSliceBlocks, p.x16);
         if (p.x16) matvec_slice_kernel<true><<<shares, 64 * kVecWaves, lds, st>>>(p);
         else matvec_slice_kernel<false><<<shares, 64 * kVecWaves, lds, st>>>(p);
         const hipError_t e = hipGetLastError();

@@ -159,7 +159,7 @@ def test_w4a16_workspace_size():
     ws = lambda M, N, K, t: kq.lib().kq_w4a16_workspace_size(M, N, K, t, ctypes.byref(n))  # noqa: E731
     assert ws(-1, 8, 64, 1) == INVALID and ws(1, 8, 40, 1) == INVALID and ws(1, 8, 64, 2) == INVALID
     assert kq.lib().kq_w4a16_workspace_size(1, 8, 64, 1, None) == NULLP
-    for M, N, K, t, used in ((0, 8, 64, 1, False), (1, 4096, 4096, 1, False), (16, 4096, 2240, 0, False), (17, 4096, 12288, 0, False),
+    for M, N, K, t, used in ((0, 8, 64, 1, False), (1, 4096, 4096, 1, False), (16, 4096, 1152, 0, False), (17, 4096, 12288, 0, False),
                              (16, 4097, 12288, 0, True), (16, 4096, 12288, 1, True), (1, 1, 1 << 20, 1, True)):
         assert ws(M, N, K, t) == SUCCESS and (n.value > 0) == used, (M, N, K, t)
         assert not used or n.value >= 4 * M * N * (K // 512)
