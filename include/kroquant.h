@@ -412,7 +412,7 @@ typedef struct kq_kv_cache {
  * way (rounded to nearest, ties to even).
  *   k, v   [T, heads, d] of dtype, element (t, h, 0) at t * k_token + h * k_head
  *   slots  device int64 [T].  A token whose slot is outside the cache is left
- *          out.  A slot given twice holds eights of columns of either token.
+ *          out.  What a slot holds that is given twice is unspecified.
  * As for the quantizers, inputs must be finite.  Arrays are aligned to their
  * elements.  T = 0 is a no-op.  Enqueued on `stream`; no allocation, no
  * synchronization.
@@ -449,7 +449,7 @@ kq_status kq_paged_attention_workspace_size(int64_t B, int64_t q_heads, int64_t 
  *   workspace   device, 16-byte aligned, kq_paged_attention_workspace_size bytes; its
  *               contents are scratch between calls
  * What the cache holds behind a sequence's tokens or before its window does not matter
- * (NaN among it).  Sums are in 32 bits and in a fixed order for given lengths.  B is at
+ * (NaN among it); q is finite.  Sums are in 32 bits and in a fixed order for given lengths.  B is at
  * most 2^20, q_heads 65535, a sequence's tokens 2^31 - 64.  B = 0 is a no-op.  Enqueued on
  * `stream`; no allocation, no synchronization.
  */
@@ -465,7 +465,7 @@ kq_status kq_w4a16_workspace_size(int64_t M, int64_t N, int64_t K, kq_dtype x_dt
  * kq_w4a16_linear -- kq_mxfp4_linear for a few rows whose activations are not
  * quantized (a decoding loop's):
  *     out = residual + gate act(x deq(B)^T + bias)
- *   x          [M, K] of x_dtype, row stride ldx >= K elements
+ *   x          [M, K] of x_dtype, row stride ldx >= K elements; out does not overlap it
  *   workspace  device, 16-byte aligned, kq_w4a16_workspace_size bytes, scratch between
  *              calls; or NULL, which is slower where that size is not 0
  *   others     as for kq_mxfp4_linear

@@ -948,6 +948,8 @@ def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=
         out_dtype = residual.dtype
     out, ldo = _linear_out(out, M, cols, out_dtype, dev)
     ldr = 0 if residual is None else _rows_of(residual, (M, cols), "residual", dev, out.dtype)
+    if _overlap(x, out) or x.data_ptr() == out.data_ptr() and out.numel():
+        raise ValueError("out overlaps x")
     if workspace is None:
         with torch.cuda.device(dev), _scratch_of(stream, dev):
             workspace = w4a16_workspace(M, N, K, x.dtype, dev)

@@ -113,6 +113,24 @@ __device__ __forceinline__ float query_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The same over a wave.
+template <int CTRL>
+__device__ __forceinline__ float row_other(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, row_other<0x128>(v));  // row_ror 8, 4, 2, 1: every lane of a row of 16 has the row's
+    v = fmaxf(v, row_other<0x124>(v));
+    v = fmaxf(v, row_other<0x122>(v));
+    return query_max(fmaxf(v, row_other<0x121>(v)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += row_other<0x128>(v);
+    v += row_other<0x124>(v);
+    v += row_other<0x122>(v);
+    return query_sum(v + row_other<0x121>(v));
+}
+
 constexpr float kLowest = -3.402823466e38f;
 
 // A uniform read of an array that the kernel does not write, by a scalar load.
@@ -261,8 +279,12 @@ __device__ __forceinline__ int value_column(int n, int i) {
 
 #define KQ_INLINE __attribute__((always_inline))
 
+// Waves of a SIMD that registers are kept for.
+template <CacheFormat F, int DC, bool B16>
+constexpr int kWavesHeld = !B16 ? 1 : DC > 128 ? 2 : F == CacheFormat::Mxfp4 || DC <= 64 ? 3 : 2;
+
 template <CacheFormat F, int DC, bool B16, bool FULL>
-__global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(kAttnThreads, (kWavesHeld<F, DC, B16>)) void attn_kernel(AttnParams p) {
     typedef Tile<F, DC, FULL> T;
     constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
     constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;  // tiles that a wave has loaded or is loading
@@ -277,9 +299,9 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
     const int rows = min(p.group - first_row, kRowTile), head = h * p.group + first_row;
     const int64_t heads = (int64_t)c.heads * p.group;
     const typename T::Lane lanes(c);
-    for (; run.tiles > 0; ++run.b, run.skip = 0) {
+    for (; run.tiles > 0; run.skip = 0) {
     // a piece: a sequence's tiles in this run, from `done` on
-    const Span span(((const_i32_ptr)p.lengths)[run.b], p.max_tokens, p.window);
+    const Span span(run.length, p.max_tokens, p.window);
     const int done = max(run.skip - kPieceTiles, 0), left = span.tiles() - done, before = max(kPieceTiles - run.skip, 0);
     const int tiles = run.tiles < left + before ? (int)run.tiles - before : left;
     run.tiles -= tiles + before;
@@ -449,6 +471,8 @@ __global__ __launch_bounds__(kAttnThreads, B16 ? 2 : 1) void attn_kernel(AttnPar
             }
         }
     }
+    if (run.tiles <= 0) break;
+    run.length = ((const_i32_ptr)p.lengths)[++run.b];
     __syncthreads();  // the next piece's waves write where these read
     }
 }
@@ -469,22 +493,32 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnParams p) {
     const f32x2* const stats = reinterpret_cast<const f32x2*>(p.stats);
     const int columns = d / 4, at = threadIdx.x / columns, column = threadIdx.x - at * columns, step = kJoinThreads / columns;
     const f32x4* const from = reinterpret_cast<const f32x4*>(p.partial) + column;
+    const bool busy = at < step;
+    auto load = [&](int i, f32x4* v, float* m) KQ_INLINE {
+        *v = from[piece(i) * columns];
+        *m = stats[piece(i)][0];
+    };
+    f32x4 now = {0.f, 0.f, 0.f, 0.f};
+    float most = kLowest;
+    if (busy && at < count) load(at, &now, &most);  // in flight while the maximum is found
     // every wave has the maximum of all pieces
     float top = kLowest, total = 0.f;
     for (int i = lane; i < count; i += 64) top = fmaxf(top, stats[piece(i)][0]);
-    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    top = wave_max(top);
     if (wave == 0) {
         for (int i = lane; i < count; i += 64) {
             const f32x2 s = stats[piece(i)];
             total += s[1] * __builtin_amdgcn_exp2f(s[0] - top);
         }
-        for (int k = 1; k < 64; k <<= 1) total += __shfl_xor(total, k);
+        total = wave_sum(total);
     }
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (at < step) {
+    f32x4 v = now * __builtin_amdgcn_exp2f(most - top);
+    if (busy) {
 #pragma unroll 4
-        for (int i = at; i < count; i += step)
-            v += from[piece(i) * columns] * __builtin_amdgcn_exp2f(stats[piece(i)][0] - top);
+        for (int i = at + step; i < count; i += step) {
+            load(i, &now, &most);
+            v += now * __builtin_amdgcn_exp2f(most - top);
+        }
     }
     __shared__ f32x4 sums[kJoinThreads];
     __shared__ float all;

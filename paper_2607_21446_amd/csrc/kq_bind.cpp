@@ -939,6 +939,7 @@ PyObject* w4a16_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
         int64_t ldo, ldr = 0;
         if (!linear_out(v[7], v[8], type, M, cols, dev, out, &ldo, &type)) return nullptr;
         if (res && (ldr = row_stride(res, M, cols, type, dev)) < 0) return nullptr;
+        if (out.given && tensor(v[7])->storage().data() == x->storage().data()) return nullptr;  // (they may overlap)
         size_t bytes = 0;
         at::Tensor made;
         void* work = nullptr;

@@ -62,6 +62,7 @@ __host__ __device__ __forceinline__ int64_t page_of(int32_t entry, int64_t pages
 // A workgroup's run: from tile `skip` - kPieceTiles of sequence b on, `tiles` in all (0: none).
 struct Run {
     int b;
+    int length;  // its tokens, as given
     int skip;
     int64_t tiles;
     int64_t each;  // of every run
@@ -86,7 +87,8 @@ __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_am
 // 2^32: a sequence of 2^31 - 64 tokens has 2^26 - 2); one where there are no more than 64.
 __device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, double inverse, int x) {
     const int lane = threadIdx.x & 63;
-    auto tiles = [&](int b) __attribute__((always_inline)) { return b < B ? (uint32_t)(Span(lengths[b], max_tokens, window).tiles() + kPieceTiles) : 0u; };
+    int length = lane < B ? lengths[lane] : 0;
+    auto tiles = [&](int b) __attribute__((always_inline)) { return b < B ? (uint32_t)(Span(length, max_tokens, window).tiles() + kPieceTiles) : 0u; };
     uint32_t n = tiles(lane), upto;
     uint64_t total = 0;
     for (int b0 = 0;;) {
@@ -94,14 +96,16 @@ __device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t m
         total += (uint32_t)lane_value((int)upto, 63);
         b0 += 64;
         if (b0 >= B) break;
+        length = b0 + lane < B ? lengths[b0 + lane] : 0;
         n = tiles(b0 + lane);
     }
-    Run r{0, 0, 0, run_tiles(total, inverse)};
+    Run r{0, 0, 0, 0, run_tiles(total, inverse)};
     const uint64_t from = (uint64_t)x * (uint64_t)r.each;
     if (from >= total) return r;
     uint64_t before = 0;
     for (int b0 = 0; b0 < B; b0 += 64) {
         if (B > 64) {
+            length = b0 + lane < B ? lengths[b0 + lane] : 0;
             n = tiles(b0 + lane);
             upto = wave_scan(n);
         }
@@ -109,6 +113,7 @@ __device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t m
         if (here) {
             const int at = __ffsll((unsigned long long)here) - 1;
             r.b = b0 + at;
+            r.length = lane_value(length, at);
             r.skip = (int)(from - before - (uint32_t)(lane_value((int)upto, at) - lane_value((int)n, at)));
             r.tiles = (int64_t)(total - from) < r.each ? (int64_t)(total - from) : r.each;
             return r;

@@ -105,7 +105,8 @@ int main(int argc, char** argv) {
             } while (wave::turn[wave::kLanes - 1] != last);
             const kq::Run& r = result[0];
             for (int l = 1; l < wave::kLanes; ++l)
-                if (result[l].b != r.b || result[l].skip != r.skip || result[l].tiles != r.tiles || result[l].each != r.each) return 4;
+                if (result[l].b != r.b || result[l].length != r.length || result[l].skip != r.skip || result[l].tiles != r.tiles || result[l].each != r.each) return 4;
+            if (r.tiles && r.length != lengths[r.b]) return 5;
             printf("%d %d %lld %lld\n", r.b, r.skip, (long long)r.tiles, (long long)r.each);
         }
     }

@@ -769,6 +769,17 @@ def test_w4a16_onto_its_residual_and_none():
         assert torch.equal(kq.w4a16_linear(x[m:m + 1], *w, out_dtype=FP32)[0], all_[m])
 
 
+def test_w4a16_out_beside_and_over_x():
+    g = _gen(35)
+    w = _codes(g, 64, 64)
+    both = _randn(g, 4, 128, dtype=BF16)
+    want = kq.w4a16_linear(both[:, :64].contiguous(), *w)
+    assert torch.equal(kq.w4a16_linear(both[:2, :64], *w, out=both[2:, 64:]), want[:2])  # one array, apart
+    for bad in (both[:, :64], both[:, 32:96], both[1:, 64:]):
+        with pytest.raises(ValueError, match="overlaps"):
+            kq.w4a16_linear(both[:len(bad), :64], *w, out=bad)
+
+
 def test_w4a16_refusals():
     g = _gen(34)
     x, (c, s) = _randn(g, 4, 64, dtype=BF16), _codes(g, 6, 64)
