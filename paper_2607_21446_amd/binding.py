@@ -680,13 +680,18 @@ def _heads_of(t, name, shape=None, device=None, dtype=None, written=False):
 
 
 def _overlap(a, b):
-    """Whether two arrays of one layout share memory without being the same."""
-    if a.data_ptr() == b.data_ptr() and a.stride() == b.stride():
+    """Whether two arrays of one number of rows may share memory without being the same."""
+    if not a.numel() or not b.numel() or a.data_ptr() == b.data_ptr() and a.stride() == b.stride() and a.shape == b.shape:
         return False
-    if not a.numel() or not b.numel():
+    row = lambda t: t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape[1:], t.stride()[1:])))  # noqa: E731
+    step = lambda t: t.element_size() * t.stride(0)  # noqa: E731
+    end = lambda t: t.data_ptr() + (t.shape[0] - 1) * step(t) + row(t)  # noqa: E731
+    if a.data_ptr() >= end(b) or b.data_ptr() >= end(a):
         return False
-    end = lambda t: t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))  # noqa: E731
-    return a.data_ptr() < end(b) and b.data_ptr() < end(a)
+    if step(a) != step(b) or not step(a):
+        return True
+    at = (b.data_ptr() - a.data_ptr()) % step(a)  # columns side by side of wider rows share none
+    return at < row(a) or at + row(b) > step(a)
 
 
 def _rope(name, x, positions, axes, theta, pairing, freqs, backward, out, out_name, stream):
@@ -697,6 +702,8 @@ def _rope(name, x, positions, axes, theta, pairing, freqs, backward, out, out_na
     xs = _heads_of(x, name)
     axes = tuple(int(a) for a in ((axes,) if isinstance(axes, int) else axes))
     T, H, D = x.shape
+    if not all(0 < a <= D for a in axes):
+        raise ValueError(f"axes must be positive and at most {D}, got {axes}")
     if positions.dtype not in _POSITIONS:
         raise TypeError(f"positions must be int32, int64 or float32, got {positions.dtype}")
     if positions.device != x.device:
@@ -902,7 +909,7 @@ def paged_attention(q, cache, page_table, lengths, scale=None, window=None, out=
     with guard:
         _check(lib().kq_paged_attention(_ptr(q), _FLOATS[q.dtype], B, Hq, *qs, ctypes.byref(c), _ptr(page_table),
                                         page_table.stride(0) if B > 1 else page_table.shape[1], page_table.shape[1], _ptr(lengths),
-                                        d ** -0.5 if scale is None else float(scale), window or 0, _ptr(out), *os_, _ptr(lse),
+                                        d ** -0.5 if scale is None else float(scale), min(window or 0, 2 ** 63 - 1), _ptr(out), *os_, _ptr(lse),
                                         _ptr(workspace), workspace.numel(), st), "kq_paged_attention")
     return out if lse is None else (out, lse)
 
@@ -948,7 +955,7 @@ def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=
         out_dtype = residual.dtype
     out, ldo = _linear_out(out, M, cols, out_dtype, dev)
     ldr = 0 if residual is None else _rows_of(residual, (M, cols), "residual", dev, out.dtype)
-    if _overlap(x, out) or x.data_ptr() == out.data_ptr() and out.numel():
+    if _overlap(x, out) or out.numel() and x.data_ptr() == out.data_ptr():
         raise ValueError("out overlaps x")
     if workspace is None:
         with torch.cuda.device(dev), _scratch_of(stream, dev):

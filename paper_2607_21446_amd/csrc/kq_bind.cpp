@@ -378,8 +378,9 @@ bool number(PyObject* o, float* v) {
 
 bool small_int(PyObject* o, int* v) {
     if (!PyLong_CheckExact(o)) return false;
-    *v = (int)PyLong_AsLong(o);
-    return true;
+    const long n = PyLong_AsLong(o);
+    *v = (int)n;
+    return *v == n && !(n == -1 && PyErr_Occurred());
 }
 
 bool float_dtype(PyObject* o, at::ScalarType* t) {
@@ -700,7 +701,7 @@ PyObject* rope(PyObject*, PyObject* const* v, Py_ssize_t n) {
         int axes[4], count = 0;
         int64_t pairs = 0;
         if (PyLong_CheckExact(v[2])) {
-            axes[count++] = (int)PyLong_AsLong(v[2]);
+            if (!small_int(v[2], &axes[count++])) return nullptr;
         } else {
             const bool list = PyList_CheckExact(v[2]);
             if (!list && !PyTuple_CheckExact(v[2])) return nullptr;
@@ -712,7 +713,6 @@ PyObject* rope(PyObject*, PyObject* const* v, Py_ssize_t n) {
                 ++count;
             }
         }
-        if (PyErr_Occurred()) return nullptr;
         for (int i = 0; i < count; ++i) pairs += axes[i] / 2;
         const bool flat = pos->dim() == 1 && count == 1;
         if (!flat && (pos->dim() != 2 || pos->size(1) != count || (count > 1 && pos->stride(1) != 1))) return nullptr;

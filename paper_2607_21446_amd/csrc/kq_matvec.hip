@@ -486,8 +486,9 @@ hipError_t launch_matvec(MatvecParams p, hipStream_t st) {
     const dim3 grid((unsigned)tiles, (unsigned)((M + kVecRows - 1) / kVecRows));
     const int64_t resident = resident_bytes(M, K, p.x16);
     if (M <= kVecRows && K >= kResidentColumns && resident <= kResidentBytes) {
-        if (p.x16) matvec_resident_kernel<true><<<grid, 64 * kVecWaves, resident, st>>>(p);
-        else matvec_resident_kernel<false><<<grid, 64 * kVecWaves, resident, st>>>(p);
+        const size_t lds = resident + (kStepBlocks - 1) * (p.x16 ? 64 : 192);  // the last step reads whole steps, and drops blocks past x
+        if (p.x16) matvec_resident_kernel<true><<<grid, 64 * kVecWaves, lds, st>>>(p);
+        else matvec_resident_kernel<false><<<grid, 64 * kVecWaves, lds, st>>>(p);
     } else if (p.partial) {
         p.columns = vec_columns(N);
         const int64_t slices = vec_slices(K), eights = (tiles + kVecWaves - 1) / kVecWaves;

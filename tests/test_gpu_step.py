@@ -187,7 +187,8 @@ def test_rope_refusals():
                 lambda: kq.rope(x, p, [64], freqs=torch.ones(32, device="cuda"))):
         with pytest.raises(TypeError):
             bad()
-    for bad in (lambda: kq.rope(x, p, [63]), lambda: kq.rope(x, p, [66]), lambda: kq.rope(x, p, [64], theta=0.0), lambda: kq.rope(x, p, [0])):
+    for bad in (lambda: kq.rope(x, p, [63]), lambda: kq.rope(x, p, [66]), lambda: kq.rope(x, p, [64], theta=0.0), lambda: kq.rope(x, p, [0]),
+                lambda: kq.rope(x, p, 2 ** 32 + 64), lambda: kq.rope(x, p, [2 ** 32 + 64]), lambda: kq.rope(x, p, [2 ** 70])):
         with pytest.raises((kq.KQError, ValueError)):
             bad()
 
@@ -775,7 +776,11 @@ def test_w4a16_out_beside_and_over_x():
     both = _randn(g, 4, 128, dtype=BF16)
     want = kq.w4a16_linear(both[:, :64].contiguous(), *w)
     assert torch.equal(kq.w4a16_linear(both[:2, :64], *w, out=both[2:, 64:]), want[:2])  # one array, apart
-    for bad in (both[:, :64], both[:, 32:96], both[1:, 64:]):
+    rows = both.clone()
+    assert torch.equal(kq.w4a16_linear(rows[:, :64], *w, out=rows[:, 64:]), want)  # columns side by side
+    assert torch.equal(kq.w4a16_linear(rows[:3, :64], *w, out=rows[1:, 64:]), want[:3])
+    assert torch.equal(rows[:, :64], both[:, :64])
+    for bad in (both[:, :64], both[:, 32:96], both[1:, :64], both.view(8, 64)[1:5]):
         with pytest.raises(ValueError, match="overlaps"):
             kq.w4a16_linear(both[:len(bad), :64], *w, out=bad)
 
