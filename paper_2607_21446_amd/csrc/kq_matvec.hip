@@ -8,7 +8,10 @@
 // row, which has one scale.  x in 32 bits goes in as three bf16 terms (8 + 8 + 8
 // bits: exact).
 //
-// Bound by the weight's read.  Three forms, by what x takes:
+// Bound by the weight's read where that is 25 MB and more (one bf16 row through
+// 4096 x 12288: 7.1 us, 3.8 TB/s), by a launch's and its loads' latencies below it
+// (4096 x 4096: 3.9 us), and with 16 rows in 32 bits by LDS (below).  Three forms,
+// by what x takes:
 //   narrow    K below 2048: a workgroup's waves take the columns of 16 rows in
 //             turn, x as the operands need it; also whatever fits no other form;
 //   resident  all of x's rows (16 at most) fit in LDS: as above with x in LDS,
@@ -39,6 +42,7 @@ constexpr int kVecRows = 16;   // of a workgroup, of the weight and of x
 constexpr int kVecWaves = 8;   // of a workgroup
 constexpr int kStepBlocks = 4;    // of a wave's step: 128 columns
 constexpr int kSliceBlocks = 16;  // of a slice: 512 columns
+constexpr int kSumThreads = 64;   // of the slices' second launch
 constexpr int kAhead = 2;           // steps that a wave has loaded or is loading
 constexpr int kResidentBytes = 136 << 10;
 constexpr int kResidentColumns = 2048;  // from here on: one row through 1152 x 1152 took 3.1 us for 2.7
@@ -89,45 +93,75 @@ __device__ __forceinline__ bf16x8 weight_operand(uint32_t c, float scale) {
         bf16x8, u32x4v{e2m1_pair<0>(c, scale), e2m1_pair<1>(c, scale), e2m1_pair<2>(c, scale), e2m1_pair<3>(c, scale)});
 }
 
-__device__ __forceinline__ float value_of(const void* p, int is16, int64_t at) {
-    return is16 ? bf16_low(static_cast<const uint16_t*>(p)[at]) : static_cast<const float*>(p)[at];
-}
+// What the epilogue of an element (of two of the weight's rows with Swiglu) reads beside the sums, as stored.  Loaded before
+// the sums are made.
+struct Beside {
+    uint32_t bias[2], gate, residual;
+    static __device__ __forceinline__ uint32_t at(const void* p, int is16, int64_t i) {
+        return is16 ? static_cast<const uint16_t*>(p)[i] : static_cast<const uint32_t*>(p)[i];
+    }
+    static __device__ __forceinline__ float value(uint32_t v, int is16) { return __uint_as_float(is16 ? v << 16 : v); }
+    // Of row m of x and row n of the weight (n even with Swiglu).
+    __device__ __forceinline__ void load(const LinearParams& l, int64_t m, int64_t n) {
+        const bool two = l.act == Act::Swiglu;
+        if (l.bias) {
+            bias[0] = at(l.bias, l.vec16, n);
+            if (two) bias[1] = at(l.bias, l.vec16, n + 1);
+        }
+        if (two) n >>= 1;
+        if (l.gate) gate = at(l.gate, l.vec16, m / l.gate_rows * l.gate_stride + n);
+        if (l.residual) residual = at(l.residual, l.out16, m * l.ldr + n);
+    }
+};
 
-// The result of `sum`, the products of row m and column n (and n + 1 with Swiglu, n even).
+// The result of the sums of row m of x and row n (and n + 1 with Swiglu, n even) of the weight.
 template <Act A>
-__device__ __forceinline__ void finish(const LinearParams& l, int64_t m, int64_t n, float v, float u) {
-    if (l.bias) v += value_of(l.bias, l.vec16, n);
+__device__ __forceinline__ void finish(const LinearParams& l, int64_t m, int64_t n, float v, float u, const Beside& e) {
+    if (l.bias) v += Beside::value(e.bias[0], l.vec16);
     float y = activate<A>(v);
     if constexpr (A == Act::Swiglu) {
-        if (l.bias) u += value_of(l.bias, l.vec16, n + 1);
+        if (l.bias) u += Beside::value(e.bias[1], l.vec16);
         y *= u;
         n >>= 1;
     }
-    if (l.gate) y *= value_of(l.gate, l.vec16, m / l.gate_rows * l.gate_stride + n);
-    if (l.residual) y += value_of(l.residual, l.out16, m * l.ldr + n);
+    if (l.gate) y *= Beside::value(e.gate, l.vec16);
+    if (l.residual) y += Beside::value(e.residual, l.out16);
     const int64_t at = m * l.ldo + n;
     if (l.out16) static_cast<__bf16*>(l.out)[at] = (__bf16)y;
     else static_cast<float*>(l.out)[at] = y;
 }
 
+// A thread's element of a tile's result: row m of x, row n of the weight; none where m is negative.
+struct TilePlace {
+    int64_t m = -1, n = 0;
+    Beside beside;
+    __device__ __forceinline__ TilePlace(const LinearParams& l, int64_t m0, int64_t n0) {
+        const int wide = l.act == Act::Swiglu ? 2 : 1, out = kVecRows / wide, i = threadIdx.x;
+        const int64_t row = m0 + i / out, column = n0 + wide * (i % out);
+        if (i >= kVecRows * out || row >= l.g.M || column >= l.g.N) return;
+        m = row;
+        n = column;
+        beside.load(l, m, n);
+    }
+};
+
 // The waves' sums of a tile in one, and its epilogue.
-__device__ __forceinline__ void finish_tile(const LinearParams& l, int64_t m0, int64_t n0, const f32x4& acc) {
+__device__ __forceinline__ void finish_tile(const LinearParams& l, int64_t m0, int64_t n0, const f32x4& acc, const TilePlace& at) {
     __shared__ float sums[kVecWaves][kVecRows][kVecRows + 1];  // [wave][row of x][row of the weight]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int k = 0; k < 4; ++k) sums[wave][lane & 15][4 * (lane >> 4) + k] = acc[k];
     __syncthreads();
+    if (at.m < 0) return;
     with_act(l.act, [&](auto a) KQ_INLINE {
         constexpr Act A = decltype(a)::value;
-        constexpr int kWide = A == Act::Swiglu ? 2 : 1, kOut = kVecRows / kWide;
-        const int i = threadIdx.x, m = i / kOut, n = kWide * (i % kOut);
-        if (i >= kVecRows * kOut || m0 + m >= l.g.M || n0 + n >= l.g.N) return;
+        const int m = (int)(at.m - m0), n = (int)(at.n - n0);
         float v[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kWide; ++j)
+        for (int j = 0; j < (A == Act::Swiglu ? 2 : 1); ++j)
 #pragma unroll
             for (int w = 0; w < kVecWaves; ++w) v[j] += sums[w][m][n + j];
-        finish<A>(l, m0 + m, n0 + n, v[0], v[1]);
+        finish<A>(l, at.m, at.n, v[0], v[1], at.beside);
     });
 }
 
@@ -192,6 +226,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_narrow_kernel(MatvecPar
     Block<X16> a, b;  // one is worked on while the other is in flight
     int at = 4 * wave;
     if (at < blocks) a.load(codes, scales, xrow, at + g, at + g < blocks, live);
+    const TilePlace place(l, m0, n0);
     while (at < blocks) {
         const int next = at + kStep, after = next + kStep;
         if (next < blocks) b.load(codes, scales, xrow, next + g, next + g < blocks, live);
@@ -201,7 +236,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_narrow_kernel(MatvecPar
         b.add(acc);
         at = after;
     }
-    finish_tile(l, m0, n0, acc);
+    finish_tile(l, m0, n0, acc, place);
 }
 
 // ------------------------------------------------------------ x in LDS
@@ -300,6 +335,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecP
         if (b0 + stage * kStep < blocks) w[stage].load(codes, scales, b0 + stage * kStep, blocks);
     });
     stage_rows<X16>(xs, stride, static_cast<const uint8_t*>(p.x), p.ldx * (X16 ? 2 : 4), rows, 0, blocks);
+    const TilePlace place(l, 0, n0);
     __syncthreads();
     const uint8_t* const mine = xs + min(r, rows - 1) * stride + g * (kTerms<X16> * 64);
     while (b0 < blocks) {
@@ -314,7 +350,7 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_resident_kernel(MatvecP
             more = b0 < blocks;
         });
     }
-    finish_tile(l, 0, n0, acc[0] + acc[1]);
+    finish_tile(l, 0, n0, acc[0] + acc[1], place);
 }
 
 // ------------------------------------------------------------ slices
@@ -337,7 +373,7 @@ __device__ __forceinline__ void quad_transpose(uint32_t& a, uint32_t& b, uint32_
 // A slice of 16 of the weight's rows: 16 blocks, four side by side a lane.  Loads as for a step, 64 bytes of a row by four
 // neighbouring lanes: lane 4 i + q reads the block q + 4 (i / 4) of row 4 (i % 4) + k in load k, and the transpose of the four
 // loads gives lane (r, g) its own row's blocks 4 g .. 4 g + 3.  (LDS is what this form waits for, x's 48 KB a tile in 32 bits:
-// with a step's exchange it took 16.7 us, with this one 15.8.)
+// both launches took 16.7 us with a step's exchange, 15.8 with this one.)
 struct Run {
     u32x4v w[4];  // after `settle`: block 4 g + k of row r
     uint32_t s;   // their scales
@@ -367,7 +403,6 @@ struct Run {
         }
     }
 };
-
 
 // A run's products in two sums: lane (r, g)'s blocks 4 g .. 4 g + 3 of the weight, those before `left` existing, with x's
 // at `from`.
@@ -416,8 +451,10 @@ struct WeightRows {
     }
 };
 
-// Slice blockIdx.y of the columns, for every gridDim.x-th eight tiles of the weight: a wave a tile.  (Two tiles a wave, which
-// share x's reads from LDS, leave two waves a SIMD and took 18 us for 16.)
+// Slice blockIdx.y of the columns, for every gridDim.x-th eight tiles of the weight: a wave a tile.  16 rows in 32 bits through
+// 12288 x 4096 take 12.7 us, the weight's 27 MB 5.3 of them, x's reads from LDS 3.8 at least; they do not overlap, since all
+// workgroups are resident at once and do the same.  (Two tiles a wave, which share x's reads, leave two waves a SIMD and took
+// 18 us for 16, both launches; x's loads issued before the weight's 16.8 for 15.9.)
 template <bool X16>
 __global__ __launch_bounds__(64 * kVecWaves) void matvec_slice_kernel(MatvecParams p) {
     extern __shared__ uint8_t xs[];
@@ -449,11 +486,17 @@ __global__ __launch_bounds__(64 * kVecWaves) void matvec_slice_kernel(MatvecPara
     }
 }
 
-// The slices' sums in one, in order, and the epilogue: four columns a thread.
-__global__ __launch_bounds__(256) void matvec_sum_kernel(MatvecParams p, int slices) {
+// The slices' sums in one, in order, and the epilogue: four columns a thread.  (Of 24 slices of 16 x 4096: 4.5 us, 5.7 with
+// the epilogue's operands loaded after the sums; 16 loads in flight instead of 8 took 6.6.)
+__global__ __launch_bounds__(kSumThreads) void matvec_sum_kernel(MatvecParams p, int slices) {
     const LinearParams& l = p.l;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, each = p.columns / 4, m = i / each, n = 4 * (i - m * each);
+    const int64_t i = (int64_t)blockIdx.x * kSumThreads + threadIdx.x, each = p.columns / 4, m = i / each, n = 4 * (i - m * each);
     if (m >= l.g.M) return;
+    Beside beside[4];
+    const int wide = l.act == Act::Swiglu ? 2 : 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (n + k < l.g.N && k % wide == 0) beside[k].load(l, m, n + k);
     const f32x4* const from = reinterpret_cast<const f32x4*>(p.partial + m * p.columns + n);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -463,7 +506,7 @@ __global__ __launch_bounds__(256) void matvec_sum_kernel(MatvecParams p, int sli
         constexpr int kWide = A == Act::Swiglu ? 2 : 1;
 #pragma unroll
         for (int k = 0; k < 4; k += kWide)
-            if (n + k < l.g.N) finish<A>(l, m, n + k, v[k], v[k + kWide - 1]);
+            if (n + k < l.g.N) finish<A>(l, m, n + k, v[k], v[k + kWide - 1], beside[k]);
     });
 }
 
@@ -500,7 +543,7 @@ hipError_t launch_matvec(MatvecParams p, hipStream_t st) {
         else matvec_slice_kernel<false><<<shares, 64 * kVecWaves, lds, st>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        matvec_sum_kernel<<<(unsigned)((M * (p.columns / 4) + 255) / 256), 256, 0, st>>>(p, (int)slices);
+        matvec_sum_kernel<<<(unsigned)((M * (p.columns / 4) + kSumThreads - 1) / kSumThreads), kSumThreads, 0, st>>>(p, (int)slices);
     } else {
         if (p.x16) matvec_narrow_kernel<true><<<grid, 64 * kVecWaves, 0, st>>>(p);
         else matvec_narrow_kernel<false><<<grid, 64 * kVecWaves, 0, st>>>(p);
