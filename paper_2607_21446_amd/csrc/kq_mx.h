@@ -61,7 +61,7 @@ __device__ __forceinline__ u32x2v e4m3_codes(const float (&v)[8], float scale) {
     for (int k = 0; k < 2; ++k) {
         float f[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = fminf(fmaxf(v[4 * k + i], -top), top);
+        for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_fmed3f(v[4 * k + i], -top, top);
         s16x2 w = {0, 0};
         w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, f[0], f[1], scale, false);
         w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, f[2], f[3], scale, true);
