@@ -5,8 +5,8 @@
 //
 // Four lanes of eight values hold a block; its maximum is two exchanges
 // between them.  Bound by HBM, a value is read and written once: 32768 tokens
-// of 8 x 128 are read from MXFP8 in 36.4 us (203 MB), 8191 written in 13.9
-// (51 MB; the vector units are busy for two thirds of it).
+// of 8 x 128 are read from MXFP8 in 35.7 us (203 MB, 5.7 TB/s), 8191 written in
+// 13.5 (51 MB).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,30 +50,25 @@ __device__ __forceinline__ float quad_max(float v) {
     return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x4e, 0xf, 0xf, false)));  // lane ^ 2
 }
 
-// How a call's eights of values are shared out: in order of token, half (keys, values), head and column; `in` counts those
-// of a workgroup's tokens.  (In order of head first, whose codes and scales are whole lines of the cache, 32768 tokens of
-// 8 x 128 in MXFP8 took 48 us to read for 38, 8191 18.4 to write for 17.0, both
-// before the multiplications below.)  Divisions are multiplications by 2^32 / n,
-// rounded up: exact for `in` below 2048 by `each` up to 1024 (where a workgroup has several tokens), and below 2^21 by up
-// to 32 columns of eight.
-// The other multiplications are of 24 bits where their factors are (a whole 32-bit one takes four times as long, and index
-// arithmetic in 64 bits kept the vector units busy for 0.8 of a write and 0.9 of a read, 17.0 and 38.4 us).
+// How a call's eights of values are shared out: a workgroup takes keys or values (blockIdx.z: their addresses and strides are
+// uniform) of some tokens, in order of token, head and column; `in` counts its eights.  Divisions are multiplications by
+// 2^32 / n, rounded up: exact for `in` below 2048 by `each` up to 1024 (where a workgroup has several tokens), and below 2^21
+// by up to 32 columns of eight.  The other multiplications are of 24 bits where their factors are (whole ones of 32 bits take
+// four times as long).  Index arithmetic in 64 bits with keys and values in one workgroup kept the vector units busy for 0.8
+// of a write and 0.9 of a read: 17.0 and 38.4 us for the calls above.  In order of head first, whose codes and scales are
+// whole lines of the cache, they took 18.4 and 48.
 struct Shares {
-    int tokens;           // of a workgroup
-    uint32_t each, half;  // eights of a token, and of one of its halves
+    int tokens;     // of a workgroup
+    uint32_t each;  // eights of a token
     uint32_t by_each, by_columns;
 };
 struct Eight {
-    uint32_t token, head, column, place;  // place: among the half's eights of the workgroup's tokens
-    bool value;
+    uint32_t token, head, column;
     __device__ __forceinline__ Eight(const Cache& c, const Shares& sh, uint32_t in) {
         token = sh.tokens > 1 ? __umulhi(in, sh.by_each) : 0u;
-        const uint32_t r = in - __umul24(token, sh.each);
-        value = r >= sh.half;
-        const uint32_t s = value ? r - sh.half : r;
+        const uint32_t s = in - __umul24(token, sh.each);
         head = __umulhi(s, sh.by_columns);
         column = 8 * (s - __umul24(head, (uint32_t)c.d / 8));
-        place = __umul24(token, sh.half) + s;
     }
 };
 
@@ -99,8 +94,11 @@ template <CacheFormat F, bool B16>
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheCopyParams p, Shares sh) {
     const Cache& c = p.c;
     const int64_t t0 = (int64_t)blockIdx.x * sh.tokens;
-    const uint32_t n = (uint32_t)min((int64_t)sh.tokens, p.T - t0) * sh.each;  // a multiple of 8: a block's lanes stay together
-    const int64_t k0 = t0 * p.k_token, v0 = t0 * p.v_token;
+    const uint32_t n = (uint32_t)min((int64_t)sh.tokens, p.T - t0) * sh.each;  // a multiple of 4: a block's lanes stay together
+    const bool value = blockIdx.z;
+    const int64_t by_token = value ? p.v_token : p.k_token, by_head = value ? p.v_head : p.k_head;
+    const uint8_t* const from = static_cast<const uint8_t*>(value ? p.v : p.k) + t0 * by_token * (B16 ? 2 : 4);
+    uint8_t *const to = value ? c.v : c.k, *const scales = value ? c.v_scales : c.k_scales;
     for (uint32_t i = blockIdx.y * kAtOnce * kCacheThreads + threadIdx.x; i < n; i += gridDim.y * kAtOnce * kCacheThreads) {
         float v[kAtOnce][8];
         int64_t slot[kAtOnce];
@@ -109,15 +107,14 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheCopyPar
             if (i + j * kCacheThreads >= n) break;
             const Eight e(c, sh, i + j * kCacheThreads);
             slot[j] = p.slots[t0 + e.token];
-            const uint64_t token = e.value ? p.v_token : p.k_token, head = e.value ? p.v_head : p.k_head;
-            load8<B16>(e.value ? p.v : p.k, (e.value ? v0 : k0) + e.token * token + e.head * head + e.column, v[j]);
+            load8<B16>(from, e.token * (uint64_t)by_token + e.head * (uint64_t)by_head + e.column, v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (i + j * kCacheThreads >= n) break;
             const Eight e(c, sh, i + j * kCacheThreads);
             const CacheRow row(c, slot[j], e.head);
-            uint8_t* const codes = (e.value ? c.v : c.k) + (row.block * 4 + e.column / 8) * kEightBytes<F>;
+            uint8_t* const codes = to + (row.block * 4 + e.column / 8) * kEightBytes<F>;
             if constexpr (F == CacheFormat::Bf16) {
                 if (!row.in) continue;
                 u32x4v w;
@@ -133,7 +130,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheCopyPar
                 if (!row.in) continue;
                 if constexpr (F == CacheFormat::Mxfp4) *reinterpret_cast<uint32_t*>(codes) = e2m1_codes(v[j], mx_scale(s));
                 else *reinterpret_cast<u32x2v*>(codes) = e4m3_codes(v[j], mx_scale(s));
-                if (e.column % 32 == 0) (e.value ? c.v_scales : c.k_scales)[row.block + e.column / 32] = (uint8_t)s;
+                if (e.column % 32 == 0) scales[row.block + e.column / 32] = (uint8_t)s;
             }
         }
     }
@@ -145,7 +142,9 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
     const Cache& c = p.c;
     const int64_t t0 = (int64_t)blockIdx.x * sh.tokens;
     const uint32_t n = (uint32_t)min((int64_t)sh.tokens, p.T - t0) * sh.each;
-    const int64_t first = t0 * sh.half;
+    const bool value = blockIdx.z;
+    const uint8_t *const from = value ? c.v : c.k, *const scales = value ? c.v_scales : c.k_scales;
+    uint8_t* const to = static_cast<uint8_t*>(value ? p.v : p.k) + t0 * sh.each * (B16 ? 16 : 32);
     for (uint32_t i = blockIdx.y * kAtOnce * kCacheThreads + threadIdx.x; i < n; i += gridDim.y * kAtOnce * kCacheThreads) {
         int64_t slot[kAtOnce];
         bool in[kAtOnce];
@@ -161,7 +160,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
             const Eight e(c, sh, i + j * kCacheThreads);
             const CacheRow row(c, slot[j], e.head);
             in[j] = row.in;
-            const uint8_t* const codes = (e.value ? c.v : c.k) + (row.block * 4 + e.column / 8) * kEightBytes<F>;
+            const uint8_t* const codes = from + (row.block * 4 + e.column / 8) * kEightBytes<F>;
             if constexpr (F == CacheFormat::Mxfp4) {
                 q[j][0] = *reinterpret_cast<const uint32_t*>(codes);
             } else if constexpr (F == CacheFormat::Mxfp8) {
@@ -173,12 +172,11 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
 #pragma unroll
                 for (int k = 0; k < 4; ++k) q[j][k] = w[k];
             }
-            if constexpr (F != CacheFormat::Bf16) s[j] = (e.value ? c.v_scales : c.k_scales)[row.block + e.column / 32];
+            if constexpr (F != CacheFormat::Bf16) s[j] = scales[row.block + e.column / 32];
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (i + j * kCacheThreads >= n) break;
-            const Eight e(c, sh, i + j * kCacheThreads);
             u32x4v w;  // as bf16, which holds every value of these formats
             if constexpr (F == CacheFormat::Bf16) {
                 w = u32x4v{q[j][0], q[j][1], q[j][2], q[j][3]};
@@ -188,7 +186,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
                 else w = u32x4v{e4m3_pair<0>(q[j][0], sc), e4m3_pair<1>(q[j][0], sc), e4m3_pair<0>(q[j][1], sc), e4m3_pair<1>(q[j][1], sc)};
             }
             if (!in[j]) w = u32x4v{0u, 0u, 0u, 0u};
-            uint8_t* const out = static_cast<uint8_t*>(e.value ? p.v : p.k) + (first + e.place) * (B16 ? 16 : 32);
+            uint8_t* const out = to + (i + j * kCacheThreads) * (B16 ? 16u : 32u);
             if constexpr (B16) {
                 *reinterpret_cast<u32x4v*>(out) = w;
             } else {
@@ -200,19 +198,17 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
     }
 }
 
-// Tokens of a workgroup, and workgroups that share them.  A small call has fewer tokens a workgroup.
+// Tokens of a workgroup, and workgroups that share them, for keys and values.  A small call has fewer tokens a workgroup.
 dim3 cache_grid(const CacheCopyParams& p, Shares* sh) {
-    const int64_t columns = p.c.d / 8, half = p.c.heads * columns, each = 2 * half;
-    const int64_t turn = kAtOnce * kCacheThreads;
+    const int64_t columns = p.c.d / 8, each = p.c.heads * columns, turn = kAtOnce * kCacheThreads;
     sh->each = (uint32_t)each;
-    sh->half = (uint32_t)half;
     sh->by_each = (uint32_t)((0x100000000ull + each - 1) / each);
     sh->by_columns = (uint32_t)((0x100000000ull + columns - 1) / columns);
     int64_t tokens = std::max<int64_t>(1, turn / each);
-    while (tokens > 1 && (p.T + tokens - 1) / tokens < 512) tokens /= 2;
+    while (tokens > 1 && (p.T + tokens - 1) / tokens < 256) tokens /= 2;
     sh->tokens = (int)tokens;
     const int64_t share = std::min<int64_t>(65535, (tokens * each + turn - 1) / turn);
-    return dim3((unsigned)((p.T + tokens - 1) / tokens), (unsigned)share);
+    return dim3((unsigned)((p.T + tokens - 1) / tokens), (unsigned)share, 2);
 }
 
 template <CacheFormat F>
