@@ -19,6 +19,13 @@
 // permutations.  Operands of 32 bits (q, and the softmax's p in any case) go in
 // as two or three bf16 terms: p = hi + lo within 2^-17 p for a bf16 result, q
 // and p as three terms, exact to 2^-24, for a 32-bit one.
+//
+// Bound by HBM for bf16 and MXFP8 (4 x 131072 tokens, 32 query heads over 8 of
+// 128: 365 us for 2148 MB, 190 for 1107 MB, 5.9 and 5.8 TB/s), for MXFP4 by the
+// vector units, which make bf16 of the codes (570 MB in 115 us; busy for 0.57
+// of the time and the matrix cores for 0.18), and for a few thousand tokens by
+// latencies one after another: lengths, page table, tiles, the waves' join, the
+// second launch (one sequence of 1000 tokens: 8.4 + 3.6 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -151,7 +158,8 @@ struct Rows {
     }
 };
 
-// DC: columns of the matrix products, at least d; FULL: d itself.  Lanes of columns past d load the row's last ones:
+// DC: columns of the matrix products, at least d; FULL: d itself (without it, widths of 64 and 128 take 12.1 us for 8.6 and
+// 49.2 for 43.6: addresses that are not constants).  Lanes of columns past d load the row's last ones:
 // q is 0 there, and those columns of the result are not stored.
 template <CacheFormat F, int DC, bool FULL>
 struct Tile {
@@ -279,7 +287,8 @@ __device__ __forceinline__ int value_column(int n, int i) {
 
 #define KQ_INLINE __attribute__((always_inline))
 
-// Waves of a SIMD that registers are kept for.
+// Waves of a SIMD that registers are kept for.  (MXFP4, 128 columns, the longest call above: 120 us with two, 115 with three;
+// four spill.)
 template <CacheFormat F, int DC, bool B16>
 constexpr int kWavesHeld = !B16 ? 1 : DC > 128 ? 2 : F == CacheFormat::Mxfp4 || DC <= 64 ? 3 : 2;
 
@@ -287,7 +296,8 @@ template <CacheFormat F, int DC, bool B16, bool FULL>
 __global__ __launch_bounds__(kAttnThreads, (kWavesHeld<F, DC, B16>)) void attn_kernel(AttnParams p) {
     typedef Tile<F, DC, FULL> T;
     constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
-    constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;  // tiles that a wave has loaded or is loading
+    // tiles that a wave has loaded or is loading (MXFP4, 128 columns: 115 us with one, 117 with two)
+    constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;
     extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3
     __shared__ float stats[2][kAttnWaves][kRowTile];
     const Cache& c = p.c;
@@ -478,7 +488,7 @@ __global__ __launch_bounds__(kAttnThreads, (kWavesHeld<F, DC, B16>)) void attn_k
 }
 
 // The pieces of a sequence in one, a workgroup a sequence and query head: its threads take four columns each of as many pieces
-// at once as there are threads for.
+// at once as there are threads for.  3 to 5 us, of which most is the launch and three loads that wait for each other.
 constexpr int kJoinThreads = 256;
 
 template <bool B16>
