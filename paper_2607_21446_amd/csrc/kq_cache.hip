@@ -5,8 +5,8 @@
 //
 // Four lanes of eight values hold a block; its maximum is two exchanges
 // between them.  Bound by HBM, a value is read and written once: 32768 tokens
-// of 8 x 128 are read from MXFP8 in 35.7 us (203 MB, 5.7 TB/s), 8191 written in
-// 13.5 (51 MB).
+// of 8 x 128 are read from MXFP8 in 34.4 us (203 MB, 5.9 TB/s), 8191 written in
+// 12.9 (51 MB).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,13 +50,14 @@ __device__ __forceinline__ float quad_max(float v) {
     return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x4e, 0xf, 0xf, false)));  // lane ^ 2
 }
 
-// How a call's eights of values are shared out: a workgroup takes keys or values (blockIdx.z: their addresses and strides are
+// How a call's eights of values are shared out: a workgroup takes keys or values (in turn: their addresses and strides are
 // uniform) of some tokens, in order of token, head and column; `in` counts its eights.  Divisions are multiplications by
 // 2^32 / n, rounded up: exact for `in` below 2048 by `each` up to 1024 (where a workgroup has several tokens), and below 2^21
 // by up to 32 columns of eight.  The other multiplications are of 24 bits where their factors are (whole ones of 32 bits take
 // four times as long).  Index arithmetic in 64 bits with keys and values in one workgroup kept the vector units busy for 0.8
 // of a write and 0.9 of a read: 17.0 and 38.4 us for the calls above.  In order of head first, whose codes and scales are
-// whole lines of the cache, they took 18.4 and 48.
+// whole lines of the cache, they took 18.4 and 48.  With all keys before the values, both calls on data that no cache holds
+// take 55.5 us instead of 52.8.
 struct Shares {
     int tokens;     // of a workgroup
     uint32_t each;  // eights of a token
@@ -93,9 +94,9 @@ constexpr int kEightBytes = F == CacheFormat::Bf16 ? 16 : F == CacheFormat::Mxfp
 template <CacheFormat F, bool B16>
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheCopyParams p, Shares sh) {
     const Cache& c = p.c;
-    const int64_t t0 = (int64_t)blockIdx.x * sh.tokens;
+    const int64_t t0 = (int64_t)(blockIdx.x >> 1) * sh.tokens;
     const uint32_t n = (uint32_t)min((int64_t)sh.tokens, p.T - t0) * sh.each;  // a multiple of 4: a block's lanes stay together
-    const bool value = blockIdx.z;
+    const bool value = blockIdx.x & 1;
     const int64_t by_token = value ? p.v_token : p.k_token, by_head = value ? p.v_head : p.k_head;
     const uint8_t* const from = static_cast<const uint8_t*>(value ? p.v : p.k) + t0 * by_token * (B16 ? 2 : 4);
     uint8_t *const to = value ? c.v : c.k, *const scales = value ? c.v_scales : c.k_scales;
@@ -140,9 +141,9 @@ template <CacheFormat F, bool B16>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyParams p, Shares sh) {
     constexpr int kWords = kEightBytes<F> / 4;
     const Cache& c = p.c;
-    const int64_t t0 = (int64_t)blockIdx.x * sh.tokens;
+    const int64_t t0 = (int64_t)(blockIdx.x >> 1) * sh.tokens;
     const uint32_t n = (uint32_t)min((int64_t)sh.tokens, p.T - t0) * sh.each;
-    const bool value = blockIdx.z;
+    const bool value = blockIdx.x & 1;
     const uint8_t *const from = value ? c.v : c.k, *const scales = value ? c.v_scales : c.k_scales;
     uint8_t* const to = static_cast<uint8_t*>(value ? p.v : p.k) + t0 * sh.each * (B16 ? 16 : 32);
     for (uint32_t i = blockIdx.y * kAtOnce * kCacheThreads + threadIdx.x; i < n; i += gridDim.y * kAtOnce * kCacheThreads) {
@@ -208,7 +209,7 @@ dim3 cache_grid(const CacheCopyParams& p, Shares* sh) {
     while (tokens > 1 && (p.T + tokens - 1) / tokens < 256) tokens /= 2;
     sh->tokens = (int)tokens;
     const int64_t share = std::min<int64_t>(65535, (tokens * each + turn - 1) / turn);
-    return dim3((unsigned)((p.T + tokens - 1) / tokens), (unsigned)share, 2);
+    return dim3((unsigned)(2 * ((p.T + tokens - 1) / tokens)), (unsigned)share);
 }
 
 template <CacheFormat F>
