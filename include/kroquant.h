@@ -422,7 +422,7 @@ kq_status kq_kv_cache_write(const kq_kv_cache* cache, const void* k, const void*
 
 /*
  * kq_kv_cache_read -- the values that slots hold, of dtype: k, v [T, heads, d],
- * contiguous, 16-byte aligned.  Rows of slots outside the cache are zeros.
+ * contiguous, 16-byte aligned, apart.  Rows of slots outside the cache are zeros.
  * Values are exact, but for those below 2^-126, which may come as zero.
  */
 kq_status kq_kv_cache_read(const kq_kv_cache* cache, const int64_t* slots, int64_t T, void* k, void* v, kq_dtype dtype, void* stream);

@@ -848,6 +848,8 @@ def kv_cache_read(cache, slots, k=None, v=None, out_dtype=None, stream=None):
         _float(t, name, dtype)
         if tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {list(shape)} on {dev}, got {list(t.shape)} on {t.device}")
+    if T and (k.data_ptr() == v.data_ptr() or _overlap(k, v)):
+        raise ValueError("k and v overlap")
     guard, st = _at(dev, stream)
     with guard:
         _check(lib().kq_kv_cache_read(ctypes.byref(c), _ptr(slots), T, _ptr(k), _ptr(v), _FLOATS[dtype], st), "kq_kv_cache_read")

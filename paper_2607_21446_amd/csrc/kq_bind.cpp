@@ -825,6 +825,10 @@ PyObject* kv_cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
         }
         if (type != at::kFloat && type != at::kBFloat16) return nullptr;
         const int64_t T = slots->numel();
+        if (v[2] != Py_None && v[3] != Py_None) {  // (they may overlap)
+            const at::Tensor *k = tensor(v[2]), *w = tensor(v[3]);
+            if (!k || !w || k->storage().data() == w->storage().data()) return nullptr;
+        }
         Out out[2];
         for (int i = 0; i < 2; ++i) {
             if (v[2 + i] != Py_None) {

@@ -365,6 +365,20 @@ def test_cache_refusals():
             bad()
 
 
+def test_cache_read_into_one_array():
+    g = _gen(14)
+    cache = kq.kv_cache(2, 16, 2, 64)
+    x, slots = _randn(g, 6, 2, 64, dtype=BF16), torch.arange(3, device="cuda")
+    kq.kv_cache_write(cache, x[:3], x[3:], slots)
+    want = kq.kv_cache_read(cache, slots)
+    both = torch.empty_like(x)
+    got = kq.kv_cache_read(cache, slots, k=both[3:], v=both[:3])  # apart
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and got[0].data_ptr() == both[3:].data_ptr()
+    for k, v in ((both[:3], both[:3]), (both[:3], both[1:4]), (both[2:5], both[:3])):
+        with pytest.raises(ValueError, match="overlap"):
+            kq.kv_cache_read(cache, slots, k=k, v=v)
+
+
 # ------------------------------------------------------------------ attention
 
 def _filled(g, pages, size, H, d, form):
