@@ -40,9 +40,10 @@ struct Span {
     }
 };
 
-// Tiles of a run, at least total / runs; `inverse` is 1 / runs.  The result is below 2^31: runs past it stay empty.
+// Tiles of a run, at least total / runs; `inverse` is 1 / runs.  (2^20 sequences in one run: up to 2^47, in 64 bits
+// throughout; a piece is of one sequence, and below 2^27.)
 __host__ __device__ __forceinline__ int64_t run_tiles(uint64_t total, double inverse) {
-    const double c = (double)total * inverse * (1.0 + 0x1p-50);  // (total < 2^46: the product's errors are below that factor's)
+    const double c = (double)total * inverse * (1.0 + 0x1p-50);  // (total < 2^47: the product's errors are below that factor's)
     const int64_t n = (int64_t)c + ((double)(int64_t)c < c);
     return n > kLeastTiles ? n : kLeastTiles;
 }
@@ -72,7 +73,7 @@ template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp_sum(uint32_t v) {
     return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
 }
-// The sum of the lanes up to and with each.
+// The sum of the lanes up to and with each, in 32 bits.
 __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     v = dpp_sum<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8: sums up to the lane in its row of 16
     v = dpp_sum<0x112, 0xf>(v);
@@ -83,14 +84,16 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 }
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// Run x, found by each of a workgroup's waves: two passes over the lengths, 64 at a time (their tiles together are below
-// 2^32: a sequence of 2^31 - 64 tokens has 2^26 - 2); one where there are no more than 64.
+// Run x, found by each of a workgroup's waves: two passes over the lengths, 64 at a time; one where there are no more than
+// 64.  Their own tiles are added up in 32 bits, which hold those of 64 sequences at the limit of 2^31 - 64 tokens; what their
+// pieces cost beside them is a multiple of the number of sequences, added in 64 bits.
+static_assert(64 * (((int64_t(1) << 31) - 64) / kTileTokens) < int64_t(1) << 32, "64 sequences' tiles in 32 bits");
 __device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t max_tokens, int64_t window, double inverse, int x) {
     const int lane = threadIdx.x & 63;
     int length = lane < B ? lengths[lane] : 0;
-    auto tiles = [&](int b) __attribute__((always_inline)) { return b < B ? (uint32_t)(Span(length, max_tokens, window).tiles() + kPieceTiles) : 0u; };
+    auto tiles = [&](int b) __attribute__((always_inline)) { return b < B ? (uint32_t)Span(length, max_tokens, window).tiles() : 0u; };
     uint32_t n = tiles(lane), upto;
-    uint64_t total = 0;
+    uint64_t total = (uint64_t)kPieceTiles * (uint32_t)B;
     for (int b0 = 0;;) {
         upto = wave_scan(n);
         total += (uint32_t)lane_value((int)upto, 63);
@@ -109,16 +112,17 @@ __device__ __forceinline__ Run find_run(const int32_t* lengths, int B, int64_t m
             n = tiles(b0 + lane);
             upto = wave_scan(n);
         }
-        const uint64_t here = __ballot(before + upto > from);
+        // (lanes past the last sequence come after one that holds `from`)
+        const uint64_t here = __ballot(before + upto + (uint32_t)(kPieceTiles * (lane + 1)) > from);
         if (here) {
             const int at = __ffsll((unsigned long long)here) - 1;
             r.b = b0 + at;
             r.length = lane_value(length, at);
-            r.skip = (int)(from - before - (uint32_t)(lane_value((int)upto, at) - lane_value((int)n, at)));
+            r.skip = (int)(from - before - (uint32_t)(lane_value((int)upto, at) - lane_value((int)n, at)) - (uint32_t)(kPieceTiles * at));
             r.tiles = (int64_t)(total - from) < r.each ? (int64_t)(total - from) : r.each;
             return r;
         }
-        before += (uint32_t)lane_value((int)upto, 63);
+        before += (uint32_t)lane_value((int)upto, 63) + (uint64_t)(64 * kPieceTiles);
     }
     return r;
 }

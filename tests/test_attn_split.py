@@ -99,3 +99,14 @@ def test_any_lengths_stay_inside(binary, seed):
 def test_pages_stay_inside(binary, token, end, shift, entry, want):
     done = subprocess.run([binary, *map(str, (token, end, shift, entry))], capture_output=True, text=True, timeout=60)
     assert done.returncode == 0 and tuple(map(int, done.stdout.split())) == want
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 128, 200])
+@pytest.mark.parametrize("runs", [1, 8, 160])
+def test_many_of_the_longest(binary, B, runs):
+    """Sequences at the limit whose tiles, and what their pieces cost, are 2^32 and more together."""
+    for longest, window in ((2 ** 31 - 1, 0), (MOST, 0), (MOST, MOST - 5)):
+        lengths = [longest] * B
+        _check(lengths, MOST, window, runs, _split(binary, lengths, MOST, window, runs))
+    lengths = [MOST] * (B - 1) + [0]
+    _check(lengths, MOST, 0, runs, _split(binary, lengths, MOST, 0, runs))
