@@ -605,7 +605,8 @@ hipError_t launch_attn(AttnParams p, hipStream_t st) {
     p.stats = reinterpret_cast<float*>(p.workspace + round16(8 * p.B));
     p.partial = reinterpret_cast<float*>(p.workspace + round16(8 * p.B) + round16(8 * run_slots(most_runs(p.c.heads, p.group)) * heads));
     // no more runs than the longest sequences that the table holds can fill
-    const int64_t longest = (p.window > 0 ? std::min(p.window + kTileTokens - 1, p.max_tokens) : p.max_tokens) / kTileTokens + 1 + kPieceTiles;
+    const int64_t seen = p.window > 0 && p.window < p.max_tokens ? std::min(p.window + kTileTokens - 1, p.max_tokens) : p.max_tokens;
+    const int64_t longest = seen / kTileTokens + 1 + kPieceTiles;
     const int64_t most = (p.B * longest + kLeastTiles - 1) / kLeastTiles;
     hipError_t e = hipSuccess;
     switch (p.c.format) {

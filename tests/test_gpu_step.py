@@ -813,3 +813,19 @@ def test_w4a16_refusals():
                 lambda: call(x, c, s, residual=torch.ones((4, 6), device="cuda"), out=torch.ones((4, 6), device="cuda", dtype=BF16))):
         with pytest.raises(TypeError):
             bad()
+
+
+# ------------------------------------------------------------------ at the operators' limits
+
+def test_attention_of_any_large_window():
+    """A window that reaches past the table is none, to the bit: the work is cut the same way."""
+    g = _gen(45)
+    for B, form in ((1, "bf16"), (3, "mxfp4")):
+        cache = _filled(g, B * 500, 64, 2, 64, form)
+        table = torch.randperm(B * 500, generator=g, device="cuda").reshape(B, 500).to(torch.int32)
+        n = torch.tensor([32000, 77, 20001][:B], dtype=torch.int32, device="cuda")
+        q = _randn(g, B, 8, 64)
+        want, lse = kq.paged_attention(q, cache, table, n, want_lse=True)
+        for window in (32000, 2 ** 31, 2 ** 62, 2 ** 63 - 31, 2 ** 63 - 1):
+            got, l2 = kq.paged_attention(q, cache, table, n, window=window, want_lse=True)
+            assert torch.equal(got, want) and torch.equal(l2, lse), window
