@@ -166,17 +166,26 @@ hipError_t launch_rope(RopeParams p, hipStream_t st) {
         p.heads = std::max<int64_t>(least, (p.H * along + 511) / 512);
     }
     p.heads = std::min<int64_t>(p.heads, p.H);
-    const dim3 grid((unsigned)along, (unsigned)((p.H + p.heads - 1) / p.heads));
+    const unsigned across = (unsigned)((p.H + p.heads - 1) / p.heads);
     const size_t lds = std::max<size_t>(8, (size_t)p.tokens * pairs * 8);
     // four pairs a step where the halves and the rest hold whole steps: one pair a step takes 47 and 39 us for the calls above
     const bool wide = pairs % 4 == 0 && rest % 4 == 0 && aligned_rows(p);
-    if (p.is16) {
-        if (wide) launch_rope_of<true, 4>(p, grid, lds, st);
-        else launch_rope_of<true, 1>(p, grid, lds, st);
-    } else {
-        if (wide) launch_rope_of<false, 4>(p, grid, lds, st);
-        else launch_rope_of<false, 1>(p, grid, lds, st);
-    }
+    const int size = p.is16 ? 2 : 4, pos_size = p.pos_type == Position::Int64 ? 8 : 4;
+    in_launches(p.T, p.tokens, kRopeThreads, [&](int64_t from, int64_t n) {
+        RopeParams l = p;
+        l.T = n;
+        l.x = static_cast<const uint8_t*>(p.x) + from * p.x_token * size;
+        l.y = static_cast<uint8_t*>(p.y) + from * p.y_token * size;
+        l.positions = static_cast<const uint8_t*>(p.positions) + from * p.pos_stride * pos_size;
+        const dim3 grid((unsigned)((n + p.tokens - 1) / p.tokens), across);
+        if (p.is16) {
+            if (wide) launch_rope_of<true, 4>(l, grid, lds, st);
+            else launch_rope_of<true, 1>(l, grid, lds, st);
+        } else {
+            if (wide) launch_rope_of<false, 4>(l, grid, lds, st);
+            else launch_rope_of<false, 1>(l, grid, lds, st);
+        }
+    });
     return hipGetLastError();
 }
 

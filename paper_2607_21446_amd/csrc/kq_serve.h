@@ -10,6 +10,14 @@ namespace kq {
 
 // Sizes already validated by the caller, in every struct here.
 
+// A grid's threads along a dimension are counted in 32 bits; past them HIP starts fewer workgroups, without an error.  So n
+// items, `each` of them to `threads` threads, go in as many launches as it takes: launch(first item, items).
+template <class F>
+void in_launches(int64_t n, int64_t each, int64_t threads, F launch) {
+    const int64_t most = (int64_t(UINT32_MAX) / threads) * each;
+    for (int64_t at = 0; at < n; at += most) launch(at, n - at < most ? n - at : most);
+}
+
 constexpr int kRopeMaxAxes = 4;
 constexpr int64_t kRopeMaxColumns = 1024;
 

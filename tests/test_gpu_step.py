@@ -829,3 +829,17 @@ def test_attention_of_any_large_window():
         for window in (32000, 2 ** 31, 2 ** 62, 2 ** 63 - 31, 2 ** 63 - 1):
             got, l2 = kq.paged_attention(q, cache, table, n, window=window, want_lse=True)
             assert torch.equal(got, want) and torch.equal(l2, lse), window
+
+
+def test_rope_of_more_tokens_than_a_launch_holds():
+    """More than 2^24 workgroups of 256 threads, which one launch does not take: every token is turned."""
+    T, D = 2 ** 24 + 3, 258  # more than 128 pairs: a workgroup a token
+    rows = _randn(_gen(41), T + D, dtype=BF16).as_strided((T, 1, D), (1, D, 1))
+    p = (torch.arange(T, device="cuda", dtype=torch.int32) * 7 % 100003).reshape(T, 1)
+    at = torch.tensor([0, 1, 65535, 2 ** 23, 2 ** 24 - 3, 2 ** 24 - 2, 2 ** 24 - 1, 2 ** 24, 2 ** 24 + 1, T - 1], device="cuda")
+    got = kq.rope(rows, p, D)
+    assert torch.equal(got[at], kq.rope(rows[at], p[at], D))
+    assert kq.rope_backward(rows, p, D, pairing="halves", dx=got) is got
+    assert torch.equal(got[at], kq.rope_backward(rows[at], p[at], D, pairing="halves"))
+    del got
+    torch.cuda.empty_cache()
