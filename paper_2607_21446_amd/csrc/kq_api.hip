@@ -723,6 +723,8 @@ kq_status kq_kv_cache_read(const kq_kv_cache* cache, const int64_t* slots, int64
     p.T = T;
     p.k = k;
     p.v = v;
+    p.k_token = p.v_token = cache->heads * cache->d;
+    p.k_head = p.v_head = cache->d;
     p.is16 = dtype == KQ_DTYPE_BF16;
     return from_hip(kq::launch_cache_read(p, (hipStream_t)stream), "kq_kv_cache_read");
 }

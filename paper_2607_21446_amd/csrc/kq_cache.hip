@@ -199,32 +199,48 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheCopyPara
     }
 }
 
-// Tokens of a workgroup, and workgroups that share them, for keys and values.  A small call has fewer tokens a workgroup.
-dim3 cache_grid(const CacheCopyParams& p, Shares* sh) {
-    const int64_t columns = p.c.d / 8, each = p.c.heads * columns, turn = kAtOnce * kCacheThreads;
-    sh->each = (uint32_t)each;
-    sh->by_each = (uint32_t)((0x100000000ull + each - 1) / each);
-    sh->by_columns = (uint32_t)((0x100000000ull + columns - 1) / columns);
-    int64_t tokens = std::max<int64_t>(1, turn / each);
+// Tokens of a workgroup.  A small call has fewer.
+Shares cache_shares(const CacheCopyParams& p) {
+    const int64_t columns = p.c.d / 8, each = p.c.heads * columns;
+    Shares sh;
+    sh.each = (uint32_t)each;
+    sh.by_each = (uint32_t)((0x100000000ull + each - 1) / each);
+    sh.by_columns = (uint32_t)((0x100000000ull + columns - 1) / columns);
+    int64_t tokens = std::max<int64_t>(1, kAtOnce * kCacheThreads / each);
     while (tokens > 1 && (p.T + tokens - 1) / tokens < 256) tokens /= 2;
-    sh->tokens = (int)tokens;
-    const int64_t share = std::min<int64_t>(65535, (tokens * each + turn - 1) / turn);
-    return dim3((unsigned)(2 * ((p.T + tokens - 1) / tokens)), (unsigned)share);
+    sh.tokens = (int)tokens;
+    return sh;
+}
+
+// launch(params, shares, grid): workgroups for keys and values of as many tokens as a launch holds.
+template <class F>
+void cache_launches(const CacheCopyParams& p, F launch) {
+    const Shares sh = cache_shares(p);
+    const int64_t turn = kAtOnce * kCacheThreads, share = std::min<int64_t>(65535, ((int64_t)sh.tokens * sh.each + turn - 1) / turn);
+    const int64_t size = p.is16 ? 2 : 4;
+    in_launches(p.T, sh.tokens, 2 * kCacheThreads, [&](int64_t from, int64_t n) {
+        CacheCopyParams l = p;
+        l.T = n;
+        l.slots = p.slots + from;
+        l.k = static_cast<uint8_t*>(p.k) + from * p.k_token * size;
+        l.v = static_cast<uint8_t*>(p.v) + from * p.v_token * size;
+        launch(l, sh, dim3((unsigned)(2 * ((n + sh.tokens - 1) / sh.tokens)), (unsigned)share));
+    });
 }
 
 template <CacheFormat F>
 void launch_write_of(const CacheCopyParams& p, hipStream_t st) {
-    Shares sh;
-    const dim3 grid = cache_grid(p, &sh);
-    if (p.is16) cache_write_kernel<F, true><<<grid, kCacheThreads, 0, st>>>(p, sh);
-    else cache_write_kernel<F, false><<<grid, kCacheThreads, 0, st>>>(p, sh);
+    cache_launches(p, [&](const CacheCopyParams& l, const Shares& sh, dim3 grid) {
+        if (l.is16) cache_write_kernel<F, true><<<grid, kCacheThreads, 0, st>>>(l, sh);
+        else cache_write_kernel<F, false><<<grid, kCacheThreads, 0, st>>>(l, sh);
+    });
 }
 template <CacheFormat F>
 void launch_read_of(const CacheCopyParams& p, hipStream_t st) {
-    Shares sh;
-    const dim3 grid = cache_grid(p, &sh);
-    if (p.is16) cache_read_kernel<F, true><<<grid, kCacheThreads, 0, st>>>(p, sh);
-    else cache_read_kernel<F, false><<<grid, kCacheThreads, 0, st>>>(p, sh);
+    cache_launches(p, [&](const CacheCopyParams& l, const Shares& sh, dim3 grid) {
+        if (l.is16) cache_read_kernel<F, true><<<grid, kCacheThreads, 0, st>>>(l, sh);
+        else cache_read_kernel<F, false><<<grid, kCacheThreads, 0, st>>>(l, sh);
+    });
 }
 
 }  // namespace

@@ -843,3 +843,26 @@ def test_rope_of_more_tokens_than_a_launch_holds():
     assert torch.equal(got[at], kq.rope_backward(rows[at], p[at], D, pairing="halves"))
     del got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("form", ["bf16", "mxfp4"])
+def test_cache_of_more_tokens_than_a_launch_holds(form):
+    """More than 2^24 workgroups of 256 threads: tokens on both sides of where the launches meet, written and read."""
+    T, H, d = 2 ** 23 + 3, 129, 32  # more than 512 eights a token: a workgroup for its keys and one for its values
+    cache = kq.kv_cache(2, 16, H, d, format=form)
+    g = _gen(42)
+    k, v = (_randn(g, T + H * d, dtype=BF16).as_strided((T, H, d), (1, d, 1)) for _ in range(2))
+    at = torch.tensor([0, 1, 65535, 2 ** 22, 2 ** 23 - 3, 2 ** 23 - 2, 2 ** 23 - 1, 2 ** 23, 2 ** 23 + 1, T - 1], device="cuda")
+    slots = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    slots[at] = torch.arange(10, device="cuda") * 3
+    kq.kv_cache_write(cache, k, v, slots)
+    for t, held in zip((k, v), _held(cache)):
+        assert torch.equal(_at(held, slots[at], 16), _nearest(t[at], form))
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("reading so many tokens takes 139 GB")
+    got = kq.kv_cache_read(cache, slots)
+    for a, b in zip(got, kq.kv_cache_read(cache, slots[at])):
+        assert torch.equal(a[at], b) and not a[2:100].any() and not a[2 ** 23 - 100:2 ** 23 - 4].any()
+    del got, a, b
+    torch.cuda.empty_cache()
