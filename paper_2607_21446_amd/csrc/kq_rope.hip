@@ -1,9 +1,9 @@
 // Rotary positions with one to four axes, and their gradient.  Pair p of a row
 // (x_a, x_b) belongs to an axis with position t and turns by t f_p:
 //     y_a = x_a cos - x_b sin,   y_b = x_b cos + x_a sin;
-// the gradient is the rotation back.  Angles are in 64 bits until they are
-// within an eighth of a turn: a position of 10^6 at f = 1 keeps 2^-33 of a
-// radian there, where 32 bits keep 2^-4.
+// the gradient is the rotation back.  Angles, their sines and cosines are in
+// 64 bits: a position of 10^6 at f = 1 keeps 2^-33 of a radian, where 32 bits
+// keep 2^-4.  The rotation is in 32 bits.
 //
 // A workgroup makes the sines of its tokens once, in LDS, and its heads share
 // them.  Bound by HBM, an element is read and written once: 4608 x 48 x 128 in
@@ -23,18 +23,22 @@ namespace {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTableBytes = 32768;
 
-// cos and sin of z, |z| <= pi / 4, by their power series: what they leave out is below 2^-28.
-__device__ __forceinline__ void sincos_small(float z, float* s, float* c) {
-    const float w = z * z;
-    float a = fmaf(w, 1.0f / 362880.0f, -1.0f / 5040.0f);
-    a = fmaf(w, a, 1.0f / 120.0f);
-    a = fmaf(w, a, -1.0f / 6.0f);
-    *s = fmaf(z * w, a, z);
-    float b = fmaf(w, -1.0f / 3628800.0f, 1.0f / 40320.0f);
-    b = fmaf(w, b, -1.0f / 720.0f);
-    b = fmaf(w, b, 1.0f / 24.0f);
-    b = fmaf(w, b, -0.5f);
-    *c = fmaf(w, b, 1.0f);
+// cos and sin of z, |z| <= pi / 4, by their power series in 64 bits: what they leave out is below 2^-41 of them.  Rounded
+// once.  (In 32 bits, from an angle rounded to 32 bits, they were off by up to 1.5 of the last place, in the same time.)
+__device__ __forceinline__ void sincos_small(double z, float* s, float* c) {
+    const double w = z * z;
+    double a = fma(w, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+    a = fma(w, a, 1.0 / 362880.0);
+    a = fma(w, a, -1.0 / 5040.0);
+    a = fma(w, a, 1.0 / 120.0);
+    a = fma(w, a, -1.0 / 6.0);
+    *s = (float)fma(z * w, a, z);
+    double b = fma(w, 1.0 / 479001600.0, -1.0 / 3628800.0);
+    b = fma(w, b, 1.0 / 40320.0);
+    b = fma(w, b, -1.0 / 720.0);
+    b = fma(w, b, 1.0 / 24.0);
+    b = fma(w, b, -0.5);
+    *c = (float)fma(w, b, 1.0);
 }
 
 // Pair p's axis, and its frequency in quarter turns a position.
@@ -95,7 +99,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
         const double turns = position(p, (t0 + t) * p.pos_stride + axis) * f;
         const double whole = rint(turns);
         float s, c;
-        sincos_small((float)((turns - whole) * 1.57079632679489661923), &s, &c);
+        sincos_small((turns - whole) * 1.57079632679489661923, &s, &c);
         const int q = (int)(whole - 4.0 * floor(whole * 0.25));  // 0 .. 3
         const float u = q & 1 ? s : c, w = q & 1 ? c : s;
         const float cs = q == 1 || q == 2 ? -u : u, sn = q >= 2 ? -w : w;

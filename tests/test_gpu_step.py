@@ -866,3 +866,17 @@ def test_cache_of_more_tokens_than_a_launch_holds(form):
         assert torch.equal(a[at], b) and not a[2:100].any() and not a[2 ** 23 - 100:2 ** 23 - 4].any()
     del got, a, b
     torch.cuda.empty_cache()
+
+
+def test_rope_angles_are_rounded_once():
+    """Rows of (1, 0) give the table itself: cos and sin of a 64-bit angle, each rounded once to 32 bits."""
+    for axes, theta, T in (([64], 1e4, 4096), ([16, 56, 56], 1e4, 1024), ([24, 24, 24], 256.0, 2048)):
+        n = sum(axes) // 2
+        x = torch.zeros((T, 1, 2 * n), device="cuda")
+        x[..., :n] = 1.0
+        p = torch.arange(T, device="cuda").reshape(T, 1).expand(T, len(axes)).contiguous()
+        for call, sign in ((kq.rope, 1), (kq.rope_backward, -1)):
+            got = call(x, p, axes, theta=theta, pairing="halves")
+            want = _rope64(x, p, axes, theta, "halves", None, sign < 0)[0]
+            # half a step of the value; angles below 2^12 from 64-bit frequencies are within 2^-38
+            _within(got, want, U * want.abs() + 2.0 ** -37, (axes, sign))
