@@ -449,8 +449,10 @@ kq_status kq_paged_attention_workspace_size(int64_t B, int64_t q_heads, int64_t 
  *   workspace   device, 16-byte aligned, kq_paged_attention_workspace_size bytes; its
  *               contents are scratch between calls
  * What the cache holds behind a sequence's tokens or before its window does not matter
- * (NaN among it); q is finite.  Sums are in 32 bits and in a fixed order for given lengths.  B is at
- * most 2^20, q_heads 65535, a sequence's tokens 2^31 - 64.  B = 0 is a no-op.  Enqueued on
+ * (NaN among it); q is finite.  Scores, exponentials, their products with V and sums
+ * are in 32 bits whatever q's type, and sums in a fixed order for given lengths, window
+ * and sizes (max_pages among them) on one kind of GPU.  B is at most 2^20, q_heads 65535,
+ * a sequence's tokens 2^31 - 64.  B = 0 is a no-op.  Enqueued on
  * `stream`; no allocation, no synchronization.
  */
 kq_status kq_paged_attention(const void* q, kq_dtype dtype, int64_t B, int64_t q_heads, int64_t q_seq, int64_t q_head,

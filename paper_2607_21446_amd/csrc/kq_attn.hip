@@ -16,9 +16,10 @@
 // is, without an exchange between lanes.  The order of the columns in S^T's sum
 // is free, so each lane's columns of K are 16 bytes side by side; V's columns
 // that a lane loads of its eight tokens are turned into operands by byte
-// permutations.  Operands of 32 bits (q, and the softmax's p in any case) go in
-// as two or three bf16 terms: p = hi + lo within 2^-17 p for a bf16 result, q
-// and p as three terms, exact to 2^-24, for a 32-bit one.
+// permutations.  Operands of 32 bits (the softmax's p, and q of that type) go in
+// as three bf16 terms, which hold their 24 bits.  (p as two terms, within 2^-16
+// of it, for bf16 results: 46 us for 49 with 64 ragged sequences of up to 8192
+// tokens in MXFP4, 194 for 199 in the MXFP8 case below.)
 //
 // Bound by HBM for bf16 and MXFP8 (4 x 131072 tokens, 32 query heads over 8 of
 // 128: 365 us for 2148 MB, 190 for 1107 MB, 5.9 and 5.8 TB/s), for MXFP4 by the
@@ -82,8 +83,8 @@ __device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, ui
     return __builtin_bit_cast(bf16x8, u32x4v{a, b, c, d});
 }
 
-// Eight values in 32 bits as TERMS bf16 operands whose sum they are: the leading bits as they stand, what is left
-// rounded in the last.
+// Eight values in 32 bits as TERMS bf16 operands whose sum they are (three; one for values of 16 bits): the leading bits as
+// they stand, what is left rounded in the last.
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&v)[8], bf16x8 (&t)[TERMS]) {
     float f[8];
@@ -295,7 +296,7 @@ constexpr int kWavesHeld = !B16 ? 1 : DC > 128 ? 2 : F == CacheFormat::Mxfp4 || 
 template <CacheFormat F, int DC, bool B16, bool FULL>
 __global__ __launch_bounds__(kAttnThreads, (kWavesHeld<F, DC, B16>)) void attn_kernel(AttnParams p) {
     typedef Tile<F, DC, FULL> T;
-    constexpr int kQ = B16 ? 1 : 3, kP = B16 ? 2 : 3;  // terms of q and p
+    constexpr int kQ = B16 ? 1 : 3, kP = 3;  // terms of q (exact in bf16, or 32 bits) and p
     // tiles that a wave has loaded or is loading (MXFP4, 128 columns: 115 us with one, 117 with two)
     constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;
     extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3

@@ -880,3 +880,35 @@ def test_rope_angles_are_rounded_once():
             want = _rope64(x, p, axes, theta, "halves", None, sign < 0)[0]
             # half a step of the value; angles below 2^12 from 64-bit frequencies are within 2^-38
             _within(got, want, U * want.abs() + 2.0 ** -37, (axes, sign))
+
+
+@pytest.mark.parametrize("form,terms", [("bf16", 2), ("mxfp8", 3), ("mxfp4", 6)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attention_probabilities_in_32_bits(form, terms, dtype):
+    """One token's p v against tokens of p = 1 whose values cancel it: what is left shows the last bits of p, whatever the
+    result's type."""
+    g = _gen(44)
+    B, d = 160, 32
+    k = torch.zeros((B, 16, 1, d), device="cuda")
+    k[:, terms, 0, 0] = -torch.rand(B, generator=g, device="cuda")
+    k = _nearest(k, form)
+    v = torch.zeros((B, 16, 1, d), dtype=torch.float64, device="cuda")
+    v[:, terms] = _nearest(torch.rand((B, 1, d), generator=g, device="cuda") + 1.0, form)
+    p = torch.exp(k[:, terms, :, :1])
+    left = -p * v[:, terms]
+    for i in range(terms):
+        v[:, i] = _nearest(left, form)
+        left = left - v[:, i]
+    cache = kq.kv_cache(B, 16, 1, d, format=form)
+    kq.kv_cache_write(cache, k.reshape(-1, 1, d).float(), v.reshape(-1, 1, d).float(), torch.arange(16 * B, device="cuda"))
+    q = torch.zeros((B, 1, d), dtype=dtype, device="cuda")
+    q[..., 0] = 1.0
+    got = kq.paged_attention(q, cache, torch.arange(B, dtype=torch.int32, device="cuda")[:, None],
+                             torch.full((B,), terms + 1, dtype=torch.int32, device="cuda"), scale=1.0)
+    total = terms + p
+    want = (v[:, :terms].sum(1) + p * v[:, terms]) / total
+    size = (v[:, :terms].abs().sum(1) + p * v[:, terms].abs()) / total
+    # the score is one product: its scale and its rounding, U each of up to 1.45 and by ln 2; the exponential 2 U; three terms
+    # of each p, added with 2 U at most
+    err = (2 * 1.5 + 2 + 2 * 3 * (terms + 1)) * U * size
+    _within(got, want, err + _stored(want, dtype) + _stored(err, dtype), form)
