@@ -826,7 +826,7 @@ def test_attention_of_any_large_window():
         n = torch.tensor([32000, 77, 20001][:B], dtype=torch.int32, device="cuda")
         q = _randn(g, B, 8, 64)
         want, lse = kq.paged_attention(q, cache, table, n, want_lse=True)
-        for window in (32000, 2 ** 31, 2 ** 62, 2 ** 63 - 31, 2 ** 63 - 1):
+        for window in (32000, 2 ** 31, 2 ** 62, 2 ** 63 - 31, 2 ** 63 - 1, 2 ** 70):
             got, l2 = kq.paged_attention(q, cache, table, n, window=window, want_lse=True)
             assert torch.equal(got, want) and torch.equal(l2, lse), window
 
@@ -912,3 +912,83 @@ def test_attention_probabilities_in_32_bits(form, terms, dtype):
     # of each p, added with 2 U at most
     err = (2 * 1.5 + 2 + 2 * 3 * (terms + 1)) * U * size
     _within(got, want, err + _stored(want, dtype) + _stored(err, dtype), form)
+
+
+@pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])
+def test_cache_rounding_at_the_smallest_scale(form):
+    """Blocks of scale byte 0 (units of 2^-127): borders between elements and saturation, where values are normal in 32 bits."""
+    grid = torch.tensor(E2M1).double() if form == "mxfp4" else torch.unique(torch.cat(
+        [torch.arange(8) * 2.0 ** -9, ((1 + torch.arange(8) / 8) * torch.exp2(torch.arange(-6.0, 9)[:, None])).flatten()])).double()
+    grid = grid[grid <= 448]
+    edge = (grid[1:] + grid[:-1]) / 2
+    v = torch.cat([grid, edge, edge * (1 + 2.0 ** -20), edge * (1 - 2.0 ** -20), torch.tensor([7.5, 7.99] if form == "mxfp4" else [464.0, 480.0, 496.0, 511.0])])
+    v = v[(v >= 2) | (v == 0)]  # 2^-126 and above
+    v = torch.cat([v, -v])
+    v = torch.nn.functional.pad(v, (0, -len(v) % 31)).reshape(-1, 31)
+    blocks = []
+    for lead in ([4.0, 2.0] if form == "mxfp4" else [256.0, 2.0, 5.0]):  # the largest magnitude's binade, and below it
+        blocks.append(torch.cat([torch.full((len(v), 1), lead).double(), v], 1))
+    x = (torch.cat(blocks) * 2.0 ** -127).reshape(-1, 1, 32).float().cuda()
+    assert ((x == 0) | (x.abs() >= 2.0 ** -126)).all()
+    cache = kq.kv_cache(-(-len(x) // 16), 16, 1, 32, format=form)
+    slots = torch.arange(len(x), device="cuda")
+    kq.kv_cache_write(cache, x, -x, slots)
+    assert not cache.k_scales.any() and not cache.v_scales.any()
+    want = _nearest(x, form)
+    held = _held(cache)
+    assert torch.equal(_at(held[0], slots, 16), want) and torch.equal(_at(held[1], slots, 16), -want)
+    for dtype in (FP32, BF16):  # below 2^-126 as they are or as zero
+        for got, sign in zip(kq.kv_cache_read(cache, slots, out_dtype=dtype), (1, -1)):
+            got = got.double()
+            assert ((got == sign * want) | ((got == 0) & (want.abs() < 2.0 ** -126))).all()
+    if form == "mxfp4":
+        codes, scales = kq.mxfp4(x[:, 0].to(BF16))
+        kq.kv_cache_write(cache, x.to(BF16), x.to(BF16), slots)
+        assert torch.equal(cache.k.transpose(1, 2).reshape(-1, 16)[:len(x)], codes) and torch.equal(cache.k_scales.reshape(-1, 1)[:len(x)], scales)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_cache_of_subnormal_values(form):
+    """Values below 2^-126 beside larger ones and on their own: held as the nearest element."""
+    g = _gen(43)
+    x = _randn(g, 48, 2, 64) * torch.exp2(torch.randint(-140, -118, (48, 2, 1), generator=g, device="cuda").double()).float()
+    assert (x.abs() < 2.0 ** -126).any() and (x.abs() >= 2.0 ** -126).any()
+    cache = kq.kv_cache(3, 16, 2, 64, format=form)
+    slots = torch.arange(48, device="cuda")
+    for dtype in (FP32, BF16):
+        y = x.to(dtype)
+        kq.kv_cache_write(cache, y, y, slots)
+        assert torch.equal(_at(_held(cache)[0], slots, 16), _nearest(y, form)), dtype
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attention_of_one_run_a_head(dtype):
+    """So many heads that each has one workgroup, which takes every sequence whole: no second launch."""
+    _check_attn("bf16", 4, 1300, 1, 32, 16, [40, 0, 7, 33], dtype)
+    _check_attn("mxfp4", 3, 1290, 2, 64, 16, [1, 100, 64], dtype, window=50)
+
+
+def test_w4a16_refuses_weights_elsewhere():
+    g = _gen(46)
+    x, (c, s) = _randn(g, 4, 64, dtype=BF16), _codes(g, 6, 64)
+    for bad in (lambda: kq.w4a16_linear(x, c.cpu(), s.cpu()), lambda: kq.w4a16_linear(x, c, s.cpu()), lambda: kq.w4a16_linear(x.cpu(), c, s)):
+        with pytest.raises(TypeError, match="device tensor"):
+            bad()
+    for bad in (lambda: kq.w4a16_linear(x, c, s, bias=torch.ones(6)), lambda: kq.w4a16_linear(x, c, s, residual=torch.ones((4, 6), dtype=BF16))):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+
+
+@pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])
+def test_attention_over_blocks_of_the_smallest_scale(form):
+    """Values in units of 2^-127 take part: one token's own, and two tokens' mean."""
+    cache = kq.kv_cache(2, 16, 1, 32, format=form)
+    v = torch.zeros((2, 16, 1, 32), device="cuda")
+    v[0, :2] = torch.tensor([2.0, 3.0, 4.0, -6.0] * 8, device="cuda") * 2.0 ** -127
+    v[1, 0] = torch.tensor([6.0, -4.0, 2.0, -2.0] * 8, device="cuda") * 2.0 ** -127
+    kq.kv_cache_write(cache, torch.zeros_like(v).reshape(-1, 1, 32), v.reshape(-1, 1, 32), torch.arange(32, device="cuda"))
+    assert not cache.v_scales.any()
+    table, n = torch.tensor([[0], [1]], dtype=torch.int32, device="cuda"), torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    for dtype in (BF16, FP32):
+        got = kq.paged_attention(torch.ones((2, 1, 32), dtype=dtype, device="cuda"), cache, table, n)
+        assert torch.equal(got[:, 0].float(), v[:, 0, 0])
