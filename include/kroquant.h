@@ -374,8 +374,8 @@ typedef enum kq_pairing {
  *   axes       HOST int [n_axes], each a positive even number
  *   theta      > 0; not used with freqs
  *   freqs      device fp64 [n] or NULL: the pairs' f, in radians a position
- * Angles are in 64 bits, the rotation in 32 with one rounding.  D is even, 2 to
- * 1024; H at most 65535.  Arrays are aligned to their elements.  T, H = 0 is a
+ * Angles, sines and cosines are in 64 bits, the latter rounded once to 32; the
+ * rotation is in 32 bits with one rounding.  D is even, 2 to 1024; H at most 65535.  Arrays are aligned to their elements.  T, H = 0 is a
  * no-op.  Enqueued on `stream`; no allocation, no synchronization.
  */
 kq_status kq_rope(const void* x, kq_dtype dtype, int64_t T, int64_t H, int64_t D, int64_t x_token, int64_t x_head,
@@ -413,16 +413,16 @@ typedef struct kq_kv_cache {
  *   k, v   [T, heads, d] of dtype, element (t, h, 0) at t * k_token + h * k_head
  *   slots  device int64 [T].  A token whose slot is outside the cache is left
  *          out.  What a slot holds that is given twice is unspecified.
- * As for the quantizers, inputs must be finite.  Arrays are aligned to their
- * elements.  T = 0 is a no-op.  Enqueued on `stream`; no allocation, no
- * synchronization.
+ * As for the quantizers, inputs must be finite.  k and v hold no part of the cache that
+ * a slot names.  Arrays are aligned to their elements.  T = 0 is a no-op.  Enqueued on
+ * `stream`; no allocation, no synchronization.
  */
 kq_status kq_kv_cache_write(const kq_kv_cache* cache, const void* k, const void* v, kq_dtype dtype, int64_t T, int64_t k_token,
                             int64_t k_head, int64_t v_token, int64_t v_head, const int64_t* slots, void* stream);
 
 /*
  * kq_kv_cache_read -- the values that slots hold, of dtype: k, v [T, heads, d],
- * contiguous, 16-byte aligned, apart.  Rows of slots outside the cache are zeros.
+ * contiguous, 16-byte aligned, apart from each other and the cache.  Rows of slots outside the cache are zeros.
  * Values are exact, but for those below 2^-126, which may come as zero.
  */
 kq_status kq_kv_cache_read(const kq_kv_cache* cache, const int64_t* slots, int64_t T, void* k, void* v, kq_dtype dtype, void* stream);
@@ -471,7 +471,8 @@ kq_status kq_w4a16_workspace_size(int64_t M, int64_t N, int64_t K, kq_dtype x_dt
  *   workspace  device, 16-byte aligned, kq_w4a16_workspace_size bytes, scratch between
  *              calls; or NULL, which is slower where that size is not 0
  *   others     as for kq_mxfp4_linear
- * The weight is read once for each 16 rows.  Products of bf16 values are exact, x in
+ * Made for up to 16 rows: the weight is read for each 16 of them, and from 17 on a call
+ * takes up to three times as long as 16 rows do.  Products of bf16 values are exact, x in
  * 32 bits takes part in full (finite values only); sums are in 32 bits, in a fixed
  * order for given sizes.  M is at most 65535 * 16.  M, N = 0 is a no-op.  Enqueued on
  * `stream`; no allocation, no synchronization.

@@ -927,8 +927,9 @@ def w4a16_linear(x, b_codes, b_scales, bias=None, act=None, gate=None, residual=
                  stream=None):
     """kq_w4a16_linear: out = residual + gate * act(x deq(B)^T + bias) for a few rows x
     [M, K] of fp32 or bf16 that are not quantized (a decoding loop's) and an MXFP4
-    weight b_codes [N, K/2], b_scales [N, K/32].  The other arguments are
-    mxfp4_linear's; a ``workspace`` of w4a16_workspace is made if it is not given (two
+    weight b_codes [N, K/2], b_scales [N, K/32].  Made for up to 16 rows: more are
+    right, but 17 take up to three times as long.  The other
+    arguments are mxfp4_linear's; a ``workspace`` of w4a16_workspace is made if it is not given (two
     calls that may run at once need one each).  Returns out."""
     a = _one_of(_ACTS, act, "act")
     r = _native().w4a16_linear(x, b_codes, b_scales, bias, a, gate, residual, out, out_dtype, workspace, stream)

@@ -22,11 +22,13 @@
 // tokens in MXFP4, 194 for 199 in the MXFP8 case below.)
 //
 // Bound by HBM for bf16 and MXFP8 (4 x 131072 tokens, 32 query heads over 8 of
-// 128: 365 us for 2148 MB, 190 for 1107 MB, 5.9 and 5.8 TB/s), for MXFP4 by the
-// vector units, which make bf16 of the codes (570 MB in 115 us; busy for 0.57
-// of the time and the matrix cores for 0.18), and for a few thousand tokens by
-// latencies one after another: lengths, page table, tiles, the waves' join, the
-// second launch (one sequence of 1000 tokens: 8.4 + 3.6 us).
+// 128: 357 us for 2148 MB, 191 for 1107 MB, 6.0 and 5.8 TB/s).  MXFP4 takes
+// about 10 us and its bytes at 5.2 TB/s (16 x 8192 tokens 37.7 us for 143 MB,
+// 64 x 4096 65 for 286): lengths, page table, q and the first tiles, the waves'
+// join and uneven ends of runs, and at 570 MB (4 x 131072) 128 to 137 us, with
+// the vector units, which make bf16 of the codes, busy for 0.6 of the time and
+// the matrix cores for 0.2.  For a few thousand tokens that first part is all,
+// with the second launch (one sequence of 1000 tokens: 9.3 + 3.9 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -159,8 +161,8 @@ struct Rows {
     }
 };
 
-// DC: columns of the matrix products, at least d; FULL: d itself (without it, widths of 64 and 128 take 12.1 us for 8.6 and
-// 49.2 for 43.6: addresses that are not constants).  Lanes of columns past d load the row's last ones:
+// DC: columns of the matrix products, at least d; FULL: d itself (without it, widths of 64 and 128 take 11.6 us for 9.0 and
+// 52.9 for 47.5: addresses that are not constants).  Lanes of columns past d load the row's last ones:
 // q is 0 there, and those columns of the result are not stored.
 template <CacheFormat F, int DC, bool FULL>
 struct Tile {
@@ -288,8 +290,8 @@ __device__ __forceinline__ int value_column(int n, int i) {
 
 #define KQ_INLINE __attribute__((always_inline))
 
-// Waves of a SIMD that registers are kept for.  (MXFP4, 128 columns, the longest call above: 120 us with two, 115 with three;
-// four spill.)
+// Waves of a SIMD that registers are kept for.  (MXFP4, 128 columns, 64 ragged sequences of up to 8192 tokens: 48 to 51 us with
+// two, 47.5 with three; four spill.)
 template <CacheFormat F, int DC, bool B16>
 constexpr int kWavesHeld = !B16 ? 1 : DC > 128 ? 2 : F == CacheFormat::Mxfp4 || DC <= 64 ? 3 : 2;
 
@@ -297,7 +299,7 @@ template <CacheFormat F, int DC, bool B16, bool FULL>
 __global__ __launch_bounds__(kAttnThreads, (kWavesHeld<F, DC, B16>)) void attn_kernel(AttnParams p) {
     typedef Tile<F, DC, FULL> T;
     constexpr int kQ = B16 ? 1 : 3, kP = 3;  // terms of q (exact in bf16, or 32 bits) and p
-    // tiles that a wave has loaded or is loading (MXFP4, 128 columns: 115 us with one, 117 with two)
+    // tiles that a wave has loaded or is loading (MXFP4, 128 columns, 64 ragged sequences: 47.5 us with one, 48 with two)
     constexpr int kAhead = F != CacheFormat::Mxfp4 && DC < 256 ? 2 : 1;
     extern __shared__ float shared[];  // [2, rows, d]: of waves 0 and 2, and 1 and 3
     __shared__ float stats[2][kAttnWaves][kRowTile];

@@ -9,11 +9,14 @@
 // bits: exact).
 //
 // Bound by the weight's read where that is 25 MB and more (one bf16 row through
-// 4096 x 12288: 7.1 us, 3.8 TB/s), by a launch's and its loads' latencies below it
-// (4096 x 4096: 3.9 us), and with 16 rows in 32 bits by LDS (below).  Three forms,
+// 4096 x 12288: 7.5 us, 3.6 TB/s), by a launch's and its loads' latencies below it
+// (4096 x 4096: 4.6 us), and with 16 rows in 32 bits by LDS (below).  Three forms,
 // by what x takes:
 //   narrow    K below 2048: a workgroup's waves take the columns of 16 rows in
-//             turn, x as the operands need it; also whatever fits no other form;
+//             turn, x as the operands need it; also whatever fits no other form,
+//             which is every call of more than 16 rows: the weight is read for
+//             each 16 of them, a row a lane (12288 x 12288 in bf16: 16 rows 25 us
+//             in slices, 17 76, 32 99, 64 194);
 //   resident  all of x's rows (16 at most) fit in LDS: as above with x in LDS,
 //             as terms, and the weight's loads 64 bytes a row;
 //   slices    they do not: workgroups take 512 columns of many rows of the

@@ -7,8 +7,10 @@
 //
 // A workgroup makes the sines of its tokens once, in LDS, and its heads share
 // them.  Bound by HBM, an element is read and written once: 4608 x 48 x 128 in
-// bf16 22.6 us, 18000 x 16 x 72 in fp32 31.6 us, 5.0 and 5.3 TB/s; one token by
-// a launch's and its loads' latencies (2.5 us).
+// bf16 22.7 us, 18000 x 16 x 72 in fp32 31.9 us, 5.0 and 5.2 TB/s; one token by
+// a launch's and its loads' latencies (2.5 us).  Rows that go a pair a step (see
+// the launch) are bound by their small accesses: 48.8 us for the second size
+// with axes of 18.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -173,7 +175,8 @@ hipError_t launch_rope(RopeParams p, hipStream_t st) {
     p.heads = std::min<int64_t>(p.heads, p.H);
     const unsigned across = (unsigned)((p.H + p.heads - 1) / p.heads);
     const size_t lds = std::max<size_t>(8, (size_t)p.tokens * pairs * 8);
-    // four pairs a step where the halves and the rest hold whole steps: one pair a step takes 47 and 39 us for the calls above
+    // Four pairs a step where rows start at multiples of 16 bytes, and the pairs that turn and the rest are multiples of four:
+    // one pair a step takes 47 and 39 us for the calls above.
     const bool wide = pairs % 4 == 0 && rest % 4 == 0 && aligned_rows(p);
     const int size = p.is16 ? 2 : 4, pos_size = p.pos_type == Position::Int64 ? 8 : 4;
     in_launches(p.T, p.tokens, kRopeThreads, [&](int64_t from, int64_t n) {

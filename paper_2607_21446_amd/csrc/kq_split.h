@@ -19,10 +19,10 @@ namespace kq {
 namespace {
 
 constexpr int kTileTokens = 32;
-constexpr int kLeastTiles = 4;   // of a run: a tile for each of a workgroup's waves (1000 tokens in bf16 took 8.4 us, with 8 9.0)
+constexpr int kLeastTiles = 4;   // of a run: a tile for each of a workgroup's waves (1000 tokens in bf16 took 8.4 us, with 8 9.0: p as two terms)
 
 // What a piece costs beside its tiles (its first loads, which nothing overlaps, and its result), in tiles: 64 ragged
-// sequences of up to 8192 tokens in MXFP4 took 70 us with 0, 59 with 4, 51 with 8, 50 with 12, 52 with 20 (48 with 12 now).
+// sequences of up to 8192 tokens in MXFP4 took 70 us with 0, 59 with 4, 51 with 8, 50 with 12, 52 with 20 (with 12 now 47 and the join's 5).
 constexpr int kPieceTiles = 12;
 
 // The tokens of a sequence that count: first .. end - 1; tiles start at multiples of 32.
