@@ -432,7 +432,10 @@ kq_status kq_mxfp4_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64
     p.gate_rows = gate ? gate_rows : 1;
     p.residual = residual;
     p.ldr = ldr;
-    return from_hip(kq::launch_mxfp4_linear(p, (hipStream_t)stream), "kq_mxfp4_linear");
+    const hipError_t e = kq::launch_mxfp4_linear(p, (hipStream_t)stream);
+    if (e == hipErrorInvalidConfiguration)
+        return fail(KQ_ERROR_UNSUPPORTED, "M = %lld and N = %lld need more workgroups than one launch holds", (long long)M, (long long)N);
+    return from_hip(e, "kq_mxfp4_linear");
 }
 
 kq_status kq_mxfp4_grouped_linear(const uint8_t* a_codes, const uint8_t* a_scales, int64_t a_rows, const int32_t* rows,
@@ -456,10 +459,12 @@ kq_status kq_mxfp4_grouped_linear(const uint8_t* a_codes, const uint8_t* a_scale
     p.offsets = offsets;
     p.experts = E;
     p.row_scale = row_scale;
-    if (kq::mxfp4_grouped_workgroups(p) > INT32_MAX)
+    const hipError_t e = kq::mxfp4_grouped_workgroups(p) > INT32_MAX ? hipErrorInvalidConfiguration
+                                                                    : kq::launch_mxfp4_linear(p, (hipStream_t)stream);
+    if (e == hipErrorInvalidConfiguration)
         return fail(KQ_ERROR_UNSUPPORTED, "R = %lld, E = %lld and N = %lld need more workgroups than one launch holds", (long long)R,
                     (long long)E, (long long)N);
-    return from_hip(kq::launch_mxfp4_linear(p, (hipStream_t)stream), "kq_mxfp4_grouped_linear");
+    return from_hip(e, "kq_mxfp4_grouped_linear");
 }
 
 static kq_status check_norm(int64_t M, int64_t d, int64_t batches, int x_dtype, int stream_dtype, int vec_dtype, int norm,

@@ -30,7 +30,7 @@ struct LinearParams {
     int stream_out = 0;  // filled in by the launcher: the output is stored past the caches
 };
 
-hipError_t launch_mxfp4_linear(LinearParams p, hipStream_t st);
+hipError_t launch_mxfp4_linear(LinearParams p, hipStream_t st);  // hipErrorInvalidConfiguration: more than one launch holds
 // Workgroups of a grouped call's largest launch, against the grid limit.
 int64_t mxfp4_grouped_workgroups(const LinearParams& p);
 

@@ -490,37 +490,49 @@ static void by_group(const LinearParams& p, F f) {
     else f(std::true_type{}, std::true_type{});
 }
 
+// Whether a launch holds that many workgroups: a grid's threads are counted in 32 bits, and past them HIP starts fewer
+// workgroups, without an error.
+static bool one_launch(int64_t groups, int64_t threads) { return groups <= int64_t(UINT32_MAX) / threads; }
+
 template <int TM, int WN, int WK, int D>
-static void launch_rows(const LinearParams& p, hipStream_t st) {
-    const dim3 grid((unsigned)((p.g.N + 16 * WN - 1) / (16 * WN) * row_tiles(p, 16 * TM)));
+static hipError_t launch_rows(const LinearParams& p, hipStream_t st) {
+    const int64_t groups = (p.g.N + 16 * WN - 1) / (16 * WN) * row_tiles(p, 16 * TM);
+    if (!one_launch(groups, 64 * WN * WK)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)groups);
     by_group(p, [&](auto grouped, auto gather) {
         hipLaunchKernelGGL((mxfp4_linear_rows_kernel<TM, WN, WK, D, decltype(grouped)::value, decltype(gather)::value>), grid,
                            dim3(64 * WN * WK), 0, st, p);
     });
+    return hipGetLastError();
 }
 
 template <int TM, int D>
-static void launch_rows_by_waves(const LinearParams& p, hipStream_t st) {
+static hipError_t launch_rows_by_waves(const LinearParams& p, hipStream_t st) {
     const int64_t split = std::min(kRowsWaves / rows_tiles(p, 16 * TM), (p.g.K + 255) / 256);
-    if (split >= 8) launch_rows<TM, 1, 8, D>(p, st);
-    else if (split >= 4) launch_rows<TM, 1, 4, D>(p, st);
-    else if (split >= 2) launch_rows<TM, 2, 2, D>(p, st);
-    else launch_rows<TM, 4, 1, D>(p, st);
+    if (split >= 8) return launch_rows<TM, 1, 8, D>(p, st);
+    if (split >= 4) return launch_rows<TM, 1, 4, D>(p, st);
+    if (split >= 2) return launch_rows<TM, 2, 2, D>(p, st);
+    return launch_rows<TM, 4, 1, D>(p, st);
 }
 
 template <int TN, int TM, int W, int D>
-static void launch_split(const LinearParams& p, hipStream_t st) {
-    const dim3 grid((unsigned)((p.g.N + 32 * TN - 1) / (32 * TN) * row_tiles(p, 32 * TM)));
+static hipError_t launch_split(const LinearParams& p, hipStream_t st) {
+    const int64_t groups = (p.g.N + 32 * TN - 1) / (32 * TN) * row_tiles(p, 32 * TM);
+    if (!one_launch(groups, 64 * W)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)groups);
     by_group(p, [&](auto grouped, auto gather) {
         hipLaunchKernelGGL((mxfp4_linear_split_kernel<TN, TM, W, D, decltype(grouped)::value, decltype(gather)::value>), grid,
                            dim3(64 * W), 0, st, p);
     });
+    return hipGetLastError();
 }
 
 template <int WN, int WM, int TN, int TM, bool PING>
-static void launch_pipe(const LinearParams& p, hipStream_t st) {
+static hipError_t launch_pipe(const LinearParams& p, hipStream_t st) {
     typedef Tile<WN, WM, TN, TM> T;
-    const dim3 grid((unsigned)((p.g.N + T::BN - 1) / T::BN * row_tiles(p, T::BM)));
+    const int64_t groups = (p.g.N + T::BN - 1) / T::BN * row_tiles(p, T::BM);
+    if (!one_launch(groups, 64 * T::WAVES)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)groups);
     const int64_t nkb = p.g.K / 32;
     const bool dma = nkb % 4 == 0 && nkb >= 16 && p.g.scales_aligned;
     by_group(p, [&](auto grouped, auto gather) {
@@ -528,6 +540,7 @@ static void launch_pipe(const LinearParams& p, hipStream_t st) {
         if (dma) hipLaunchKernelGGL((mxfp4_linear_pipe_kernel<WN, WM, TN, TM, PING, true, GR, GA>), grid, dim3(64 * T::WAVES), 0, st, p);
         else hipLaunchKernelGGL((mxfp4_linear_pipe_kernel<WN, WM, TN, TM, PING, false, GR, GA>), grid, dim3(64 * T::WAVES), 0, st, p);
     });
+    return hipGetLastError();
 }
 
 int64_t mxfp4_grouped_workgroups(const LinearParams& p) { return (p.g.N + 15) / 16 * row_tiles(p, 16); }
@@ -545,14 +558,14 @@ hipError_t launch_mxfp4_linear(LinearParams p, hipStream_t st) {
     // (141 MB) 140, 132; 12004 x 1152 x 2240 fp32, one weight (115 MB), onto the same output each time 46, 54.
     p.stream_out = touched(p) > (int64_t(128) << 20);
     switch (linear_tile_of(p)) {
-        case LinearTile::Rows16: launch_rows_by_waves<1, 3>(p, st); break;
-        case LinearTile::Rows32: launch_rows_by_waves<2, 3>(p, st); break;
-        case LinearTile::Split32: launch_split<1, 1, 8, 4>(p, st); break;
-        case LinearTile::Split64: launch_split<2, 2, 8, 2>(p, st); break;
-        case LinearTile::Pipe128: launch_pipe<2, 2, 2, 2, false>(p, st); break;
-        case LinearTile::Pipe256: launch_pipe<2, 4, 4, 2, true>(p, st); break;
+        case LinearTile::Rows16: return launch_rows_by_waves<1, 3>(p, st);
+        case LinearTile::Rows32: return launch_rows_by_waves<2, 3>(p, st);
+        case LinearTile::Split32: return launch_split<1, 1, 8, 4>(p, st);
+        case LinearTile::Split64: return launch_split<2, 2, 8, 2>(p, st);
+        case LinearTile::Pipe128: return launch_pipe<2, 2, 2, 2, false>(p, st);
+        case LinearTile::Pipe256: break;
     }
-    return hipGetLastError();
+    return launch_pipe<2, 4, 4, 2, true>(p, st);
 }
 
 }  // namespace kq

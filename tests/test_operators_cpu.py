@@ -125,3 +125,14 @@ def test_binding_names_what_is_wrong():
         kq.block_norm_backward(x, x, norm=None)
     with pytest.raises(TypeError, match="float32 or bfloat16"):
         kq.block_norm(x.half())
+
+
+@pytest.mark.parametrize("call,kw", [
+    (_linear, dict(M=(1 << 31) - 1, N=4, K=32)),  # 2^24 tiles of 128 rows, of 256 threads
+    (_grouped, dict(R=1 << 20, T=1 << 20, E=1 << 20, N=1024, ldo=1024, K=32)),  # 2^24 tiles of 64 features, of 256 threads
+    (_grouped, dict(R=1 << 22, T=1 << 22, E=8, N=1 << 22, ldo=1 << 22, K=1 << 25)),  # 2^32 tiles of 64 x 64
+])
+def test_more_threads_than_a_launch_counts(call, kw):
+    """Fewer than 2^31 workgroups whose threads pass 2^32, which a launch would start modulo 2^32."""
+    assert call(**kw) == UNSUPPORTED
+    assert b"more workgroups than one launch holds" in kq.lib().kq_last_error_detail()
